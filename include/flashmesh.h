@@ -391,6 +391,163 @@ const char* fm_strerror(int code);
  * cleared by fm_prefill.  Synchronises the stream. */
 int fm_device_status(fm_ctx* ctx);
 
+/* ------------------------------------------------------------------------------------------
+ * Trees of drafts over a paged cache
+ *
+ * The stages above verify one chain of candidates over caches that a context owns.  The calls below
+ * serve hosts that verify a tree of alternatives instead (several drafts per position, taken from
+ * the top alternatives of the draft distributions) and share cached prefixes between sequences: they
+ * work on the caller's own buffers and need no context.
+ *   fm_logprobs          log probabilities of given tokens, entropy, rank, top alternatives
+ *   fm_tree_attention    attention of a tree's nodes over a paged cache and their ancestors
+ *   fm_tree_accept       the longest path of the tree that the predictions confirm
+ *   fm_pages_*           pages for new positions, appended rows, forks, roll-back, compaction
+ *
+ * Conventions beside those at the top
+ *   - All of them only enqueue work on `stream` (a cudaStream_t; NULL = the default stream), allocate
+ *     nothing, never wait and can be captured into a graph.  The device that holds the buffers has to
+ *     be the current one.  What the host can check is checked before anything is enqueued; an error
+ *     return has enqueued nothing.
+ *   - What only the device sees (an id out of range, an exhausted pool) never leads to an access out
+ *     of bounds: the entry concerned is left as it was and, where a call has a status word, the error
+ *     is recorded there (DEV int32, 0 = none; of several the lowest code stays; the caller clears it).
+ *   - A call may be enqueued while earlier ones on the same buffers run on the same stream.  Calls on
+ *     the same fm_pages, or with the same workspace, from two streams (or two graphs that may run at
+ *     the same time) have to be ordered by the caller.
+ *   - Results depend on the arguments alone, to the last bit: the same call gives the same bits.  The
+ *     attention of a sequence in other company agrees to rounding (the split of the work follows all lengths).
+ * ------------------------------------------------------------------------------------------ */
+#define FM_BF16 0
+#define FM_FP16 1
+#define FM_FP32 2
+
+#define FM_MAX_TOP 32               /* alternatives per row of fm_logprobs                          */
+#define FM_MAX_TREE_NODES 256       /* nodes of one tree                                            */
+#define FM_MAX_SEQS 4096            /* sequences of one fm_pages, entries of one call               */
+
+/* A pool of cache pages: element i of the key of position `slot` of page `page`, head h, layer l is
+ * k[l*layer_stride + page*page_stride + h*head_stride + slot*slot_stride + i]; values alike.  Strides
+ * in elements, multiples of 8; k and v 16-byte aligned.  The same page ids serve every layer. */
+typedef struct fm_cache {
+  void* k; void* v;                 /* DEV                                                          */
+  int64_t layer_stride, page_stride, head_stride, slot_stride;
+  int32_t n_layers, n_pages, page_slots, n_kv_heads, head_dim;
+  int32_t dtype;                    /* FM_BF16 or FM_FP16                                           */
+} fm_cache;
+
+/* Which pages belong to which sequence.  All arrays DEV int32, owned by the caller; the calls keep
+ * refs[p] = number of table entries that hold page p.  The entries of a sequence are filled from the
+ * front; positions 0 .. lens-1 hold keys and values, entries behind them may be reserved already. */
+typedef struct fm_pages {
+  int32_t n_pages, page_slots, max_seqs, max_pages;
+  int32_t* table;                   /* [max_seqs, max_pages] page ids, -1 = none                    */
+  int32_t* lens;                    /* [max_seqs]                                                   */
+  int32_t* refs;                    /* [n_pages] holders of every page, 0 = free                    */
+  int32_t* status;                  /* [1]                                                          */
+  int32_t* work;                    /* [fm_pages_work_ints()] scratch, zeroed once (fm_pages_reset) */
+} fm_pages;
+size_t fm_pages_work_ints(int32_t n_pages, int32_t max_seqs);      /* 0 if a size is out of range */
+
+/* All pages free, all lengths zero; clears status and work. */
+int fm_pages_reset(const fm_pages* pages, void* stream);
+
+/* dst[i] becomes a copy of src[i], i < n: it gives up its own pages and holds those of src[i] that
+ * have positions, shared (pages reserved ahead are not shared).  Nothing is copied until one of them grows
+ * (fm_pages_reserve).  Entries with a negative src or dst are skipped.  INVALID_ARG in the status
+ * word, and the entry skipped: an id >= max_seqs, a dst that an earlier entry has too, a src that is
+ * a dst of the same call. */
+int fm_pages_fork(const fm_pages* pages, const int32_t* src /*DEV*/, const int32_t* dst /*DEV*/, int32_t n, void* stream);
+
+/* Pages for grow[i] more positions of sequence seqs[i]: afterwards the table covers lens + grow
+ * positions, and the page of the next position is the sequence's own: when it is partly filled and shared, its filled
+ * part is copied to a fresh page, in every layer (the last of several holders in one call keeps it).
+ * Free pages are handed out lowest id first, in the order of the entries, inside an entry in the
+ * order of the positions.  An entry that cannot have all its pages (too few free, or behind
+ * max_pages) gets none: CAPACITY in the status word; those behind it are still served.  Negative
+ * seqs are skipped; an id >= max_seqs or listed before: INVALID_ARG, skipped.  Copied pages are read whole up to the length. */
+int fm_pages_reserve(const fm_pages* pages, const fm_cache* cache, const int32_t* seqs /*DEV*/, const int32_t* grow /*DEV*/, int32_t n,
+                     void* stream);
+
+/* Write new keys and values behind the cache of the listed sequences and advance their lengths.
+ * Sequence seqs[i] owns the rows row_off[i] .. row_off[i+1]-1 of k_new / v_new (element j of head h
+ * of row r, layer l: k_new[l*new_layer_stride + r*new_row_stride + h*new_head_stride + j]; strides multiples of 8, 16-byte aligned).
+ * path == NULL: all its rows, in order.  Otherwise rows path[i*path_stride + 0 .. n_acc[i]-1],
+ * counted from row_off[i] (an accepted path of a tree).  max_rows: bound on the rows one sequence
+ * appends (HOST).  An entry whose pages are not all there, or are shared (no fm_pages_reserve), with a
+ * row outside its own or more rows than max_rows is skipped: BAD_STATE or INVALID_ARG in the status
+ * word; its length stays.  Ids as in fm_pages_reserve. */
+typedef struct fm_new_rows {
+  const void* k; const void* v;     /* DEV, the type of the cache                                   */
+  int64_t layer_stride, row_stride, head_stride;
+} fm_new_rows;
+int fm_pages_append(const fm_pages* pages, const fm_cache* cache, const fm_new_rows* rows, const int32_t* seqs /*DEV*/,
+                    const int32_t* row_off /*DEV [n+1]*/, const int32_t* path /*DEV or NULL*/, int32_t path_stride,
+                    const int32_t* n_acc /*DEV [n], with path*/, int32_t n, int32_t max_rows, void* stream);
+
+/* Cut sequence seqs[i] to min(lens, max(new_lens[i], 0)) positions and give back every page behind them, those
+ * reserved ahead included (0: the sequence is empty).  Ids as in fm_pages_reserve. */
+int fm_pages_truncate(const fm_pages* pages, const int32_t* seqs /*DEV*/, const int32_t* new_lens /*DEV*/, int32_t n, void* stream);
+
+/* Move the pages in use to the front of the pool: with U pages in use the k-th lowest used page with an id
+ * >= U moves to the k-th lowest free id, in every layer; table and refs follow.  used: DEV out [1] U, or NULL. */
+int fm_pages_compact(const fm_pages* pages, const fm_cache* cache, int32_t* used /*DEV*/, void* stream);
+
+/* Attention of trees of drafted tokens (one node: a single token).  The nodes of sequence i are rows
+ * row_off[i] .. row_off[i+1]-1 of q, k_new and v_new, with parent[row] the node it continues, counted
+ * from row_off[i]: an earlier node, or -1 for a node that continues the cached positions.  With
+ * len = lens[seq], depth(i) the number of a node's ancestors and position len + depth(i):
+ *   a node sees itself and its ancestors, and the cached positions s < len;
+ *   window > 0: of both only what lies less than `window` positions before it, and always the
+ *   positions s < n_prefix (conditioning).
+ * out = sum p v, p = softmax(scale q k), sums and softmax in 32 bits (p is rounded to the cache's type for its
+ * product with v); lse = log sum exp(scale q k).
+ * A parent that is no earlier node and not -1 takes its node and every node below it out of use:
+ * out 0, lse -inf; nobody sees them.  Values of positions and nodes that a row does not see have no
+ * effect on it, whatever they hold.  Rows behind row_off[n] are left as they were.  Nodes behind max_nodes, and
+ * positions behind the table or max_len, are not seen; rows of such nodes are left as they were.
+ * Nothing is appended to the cache.  Errors: INVALID_ARG (null pointer, size, stride or alignment),
+ * UNSUPPORTED (head_dim not 64 / 128, dtype), CAPACITY (workspace, batch > FM_MAX_SEQS, max_nodes > FM_MAX_TREE_NODES). */
+typedef struct fm_tree_args {
+  const void* q;                    /* DEV [rows, n_heads, head_dim], rows q_row_stride apart        */
+  const void* k_new; const void* v_new;   /* DEV [rows, n_kv_heads, head_dim], rows new_row_stride apart */
+  void* out;                        /* DEV [rows, n_heads, head_dim], rows out_row_stride apart      */
+  float* lse;                       /* DEV [rows, n_heads] or NULL                                   */
+  int64_t q_row_stride, new_row_stride, out_row_stride;   /* elements, multiples of 8; buffers 16-byte aligned */
+  const int32_t* table;             /* DEV [.., max_pages] as in fm_pages                            */
+  const int32_t* lens;              /* DEV                                                           */
+  const int32_t* seqs;              /* DEV [batch] rows of table and lens, NULL: 0 .. batch-1; a negative one has no positions */
+  const int32_t* row_off;           /* DEV [batch+1]                                                 */
+  const int32_t* parent;            /* DEV [rows]                                                    */
+  int32_t* status;                  /* DEV [1] or NULL: TIMEOUT if a bounded wait gave up            */
+  int32_t max_pages, max_seqs, batch, n_heads, max_nodes, max_len, window, n_prefix;
+  float scale;
+} fm_tree_args;
+size_t fm_tree_attention_bytes(const fm_cache* cache, const fm_tree_args* args);   /* workspace; 0 if the arguments are invalid */
+int fm_tree_attention(const fm_cache* cache, int32_t layer, const fm_tree_args* args, void* workspace /*DEV, 256-byte aligned*/,
+                      size_t workspace_bytes, void* stream);
+
+/* The longest confirmed path of every tree: from node 0 (the token already accepted, parent -1) on to the lowest
+ * child whose token is the prediction at the node, as long as there is one.  path: DEV out
+ * [batch, path_stride], node indices counted from row_off[i], then -1; n_acc: DEV out [batch]; next_tok:
+ * DEV out [batch], the prediction at the last node of the path.  A sequence without rows, or whose
+ * node 0 has a parent: n_acc 0, next_tok -1.  Nodes behind path_stride or FM_MAX_TREE_NODES are not followed. */
+int fm_tree_accept(const int32_t* tokens /*DEV [rows]*/, const int32_t* parent /*DEV*/, const int32_t* row_off /*DEV*/,
+                   const int32_t* predicted /*DEV [rows]*/, int32_t batch, int32_t* path, int32_t path_stride, int32_t* n_acc, int32_t* next_tok,
+                   void* stream);
+
+/* Scores of logits rows x (FM_FP32 / FM_BF16 / FM_FP16, `row_stride` elements apart; e.g. those of
+ * fm_verify or fm_draft), one pass over the data:
+ *   logprob[r] = x_t - log sum exp x, t = tokens[r];  rank[r] = number of entries above x_t
+ *   entropy[r] = -sum p log p (natural logarithm; an entry of -inf counts 0)
+ *   top_ids / top_logprobs [rows, top]: the largest entries, equal ones lowest id first
+ * in 32 bits.  tokens NULL, or a token outside [0, vocab): logprob -inf, rank -1.  An output may be
+ * NULL.  A row of -inf alone: logprob -inf, entropy 0, top_logprobs -inf.  A NaN or +inf in a row makes logprob, entropy
+ * and top_logprobs NaN; a NaN ranks below -inf.  Errors: INVALID_ARG (null logits, rows < 0, vocab < 1, stride < vocab, top < 0 or > vocab, dtype),
+ * CAPACITY (top > FM_MAX_TOP). */
+int fm_logprobs(const void* logits /*DEV*/, int32_t dtype, int32_t rows, int32_t vocab, int64_t row_stride, const int32_t* tokens /*DEV or NULL*/,
+                float* logprob, float* entropy, int32_t* rank, int32_t top, int32_t* top_ids, float* top_logprobs, void* stream);
+
+
 #ifdef __cplusplus
 }
 #endif

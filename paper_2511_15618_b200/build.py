@@ -7,9 +7,9 @@ import sys
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB = os.path.join(HERE, "libflashmesh.so")
-SRC = os.path.join(HERE, "csrc", "flashmesh.cu")
+SRC = [os.path.join(HERE, "csrc", f) for f in ("flashmesh.cu", "fm_ops.cu")]
 NVCC_FLAGS = ["-O3", "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo",
-              "-Xcompiler", "-fPIC", "-shared"]
+              "-Xcompiler", "-fPIC", "-shared", "--threads", "2"]
 
 
 def _sources():
@@ -26,7 +26,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
         if all(os.path.getmtime(s) <= t for s in _sources()):
             return LIB
     nvcc = os.environ.get("NVCC", "nvcc")
-    cmd = [nvcc] + NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else []) + ["-o", LIB, SRC]
+    cmd = [nvcc] + NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else []) + ["-o", LIB] + SRC
     res = subprocess.run(cmd, capture_output=True, text=True)
     if res.returncode != 0:
         sys.stderr.write(res.stdout + res.stderr)

@@ -1,0 +1,259 @@
+// C ABI of the calls that need no context: trees of drafts over a paged cache, token scores (see include/flashmesh.h).
+// The host checks the arguments, picks a kernel by sizes and types and enqueues it.
+#include "../../include/flashmesh.h"
+
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include <atomic>
+
+#include "fm_logprobs.cuh"
+#include "fm_pages.cuh"
+#include "fm_tree.cuh"
+
+namespace {
+
+constexpr int64_t MOST_SLOTS = 1 << 30;      // positions a table can hold
+constexpr int MOST_GRID = 65535;
+
+inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+inline cudaStream_t as_stream(void* s) { return reinterpret_cast<cudaStream_t>(s); }
+inline int launched() { return cudaGetLastError() == cudaSuccess ? FM_OK : FM_ERR_CUDA; }
+
+// second launch of a pair: its blocks may start while the first one's still run
+template <typename Kernel, typename... Args>
+cudaError_t launch_behind(Kernel kern, dim3 grid, int block, cudaStream_t stream, Args... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(block);
+  cfg.stream = stream;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kern, args...);
+}
+
+// the kernel may use that much shared memory on the current device (asked once per device)
+template <typename Kernel>
+bool allow_smem(Kernel kern, int bytes, std::atomic<uint64_t>& asked) {
+  int dev = -1;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0) return false;
+  if (dev < 64 && ((asked.load() >> dev) & 1)) return true;
+  if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return false;
+  if (dev < 64) asked.fetch_or(1ull << dev);
+  return true;
+}
+
+int check_pages(const fm_pages* p) {
+  if (p == nullptr || p->table == nullptr || p->lens == nullptr || p->refs == nullptr || p->status == nullptr || p->work == nullptr) return FM_ERR_INVALID_ARG;
+  if (p->page_slots < 1 || p->max_pages < 1 || fm_pages_work_ints(p->n_pages, p->max_seqs) == 0) return FM_ERR_INVALID_ARG;
+  if ((int64_t)p->max_pages * p->page_slots > MOST_SLOTS) return FM_ERR_CAPACITY;
+  return FM_OK;
+}
+
+int check_cache(const fm_cache* c) {
+  if (c == nullptr || c->k == nullptr || c->v == nullptr || !aligned16(c->k) || !aligned16(c->v)) return FM_ERR_INVALID_ARG;
+  if (c->n_layers < 1 || c->n_pages < 1 || c->page_slots < 1 || c->n_kv_heads < 1) return FM_ERR_INVALID_ARG;
+  if ((c->layer_stride | c->page_stride | c->head_stride | c->slot_stride) & 7) return FM_ERR_INVALID_ARG;
+  if (c->head_dim < 8 || c->head_dim % 8 != 0) return FM_ERR_INVALID_ARG;
+  if (c->dtype != FM_BF16 && c->dtype != FM_FP16) return FM_ERR_UNSUPPORTED;
+  if (c->n_layers > MOST_GRID / 2 - 1) return FM_ERR_CAPACITY;
+  return FM_OK;
+}
+
+int check_both(const fm_pages* p, const fm_cache* c) {
+  int rc = check_pages(p);
+  if (rc == FM_OK) rc = check_cache(c);
+  if (rc == FM_OK && (p->n_pages != c->n_pages || p->page_slots != c->page_slots)) rc = FM_ERR_INVALID_ARG;
+  return rc;
+}
+
+int check_list(const int32_t* a, const int32_t* b, int32_t n) {
+  if (n < 0 || (n > 0 && (a == nullptr || b == nullptr))) return FM_ERR_INVALID_ARG;
+  return n > FM_MAX_SEQS ? FM_ERR_CAPACITY : FM_OK;
+}
+
+pg::Geo geo_of(const fm_cache& c) {
+  pg::Geo g;
+  g.k = static_cast<char*>(c.k); g.v = static_cast<char*>(c.v);
+  g.layer = 2 * c.layer_stride; g.page = 2 * c.page_stride; g.head = 2 * c.head_stride; g.slot = 2 * c.slot_stride;
+  g.layers = c.n_layers; g.heads = c.n_kv_heads; g.row16 = c.head_dim / 8;
+  return g;
+}
+
+tr::Div div_by(int d) {
+  tr::Div v{0, 0, d};
+  if (d > 1) {
+    int l = 0;
+    while ((1ll << l) < d) ++l;
+    const int p = 31 + l;                      // n * (2^p / d rounded up) >> p is exact for n < 2^31
+    v.mul = (uint32_t)(((1ull << p) + d - 1) / d);
+    v.shift = p - 32;
+  }
+  return v;
+}
+
+int check_tree(const fm_cache* c, const fm_tree_args* t) {
+  const int rc = check_cache(c);
+  if (rc != FM_OK) return rc;
+  if (t == nullptr || t->q == nullptr || t->k_new == nullptr || t->v_new == nullptr || t->out == nullptr || t->table == nullptr || t->lens == nullptr ||
+      t->row_off == nullptr || t->parent == nullptr) return FM_ERR_INVALID_ARG;
+  if (!aligned16(t->q) || !aligned16(t->k_new) || !aligned16(t->v_new) || !aligned16(t->out)) return FM_ERR_INVALID_ARG;
+  if (t->batch < 1 || t->n_heads < 1 || t->n_heads % c->n_kv_heads != 0 || t->max_nodes < 1 || t->max_len < 0 || t->window < 0 || t->n_prefix < 0 ||
+      t->max_pages < 1 || t->max_seqs < 1) return FM_ERR_INVALID_ARG;
+  if ((t->q_row_stride | t->new_row_stride | t->out_row_stride) & 7) return FM_ERR_INVALID_ARG;
+  if (t->q_row_stride < (int64_t)t->n_heads * c->head_dim || t->out_row_stride < (int64_t)t->n_heads * c->head_dim ||
+      t->new_row_stride < (int64_t)c->n_kv_heads * c->head_dim) return FM_ERR_INVALID_ARG;
+  if (!(t->scale == t->scale) || t->scale - t->scale != 0.f) return FM_ERR_INVALID_ARG;
+  if (c->head_dim != 64 && c->head_dim != 128) return FM_ERR_UNSUPPORTED;
+  if (t->batch > FM_MAX_SEQS || t->max_nodes > FM_MAX_TREE_NODES || (int64_t)t->max_pages * c->page_slots > MOST_SLOTS) return FM_ERR_CAPACITY;
+  return FM_OK;
+}
+
+constexpr size_t DESC_BYTES = 16 * tr::CTAS + 128;
+static_assert(DESC_BYTES % 256 == 0 || DESC_BYTES < 4096, "");
+inline size_t part_bytes(int rows, int dh) { return (size_t)tr::CTAS * 2 * rows * (dh + 2) * sizeof(float); }
+
+template <typename T, int DH>
+int tree_rows16(const tr::Args& a, cudaStream_t stream) {
+  static std::atomic<uint64_t> asked{0};
+  using CF = tr::Rows16<DH>;
+  if (!allow_smem(tr::rows16_kernel<T, DH>, CF::bytes(FM_MAX_SEQS), asked)) return FM_ERR_CUDA;
+  tr::rows16_kernel<T, DH><<<tr::CTAS, CF::THREADS, CF::bytes(a.batch), stream>>>(a);
+  if (cudaGetLastError() != cudaSuccess) return FM_ERR_CUDA;
+  return launch_behind(tr::merge_kernel<T, DH, 16>, dim3(tr::CTAS, 4), 256, stream, a) == cudaSuccess ? FM_OK : FM_ERR_CUDA;
+}
+
+template <typename T>
+int score_rows(const lp::Args& a, cudaStream_t stream) {
+  if (a.vocab <= 2048) lp::rows_kernel<T, 128><<<a.rows, 128, 0, stream>>>(a);
+  else lp::rows_kernel<T, 512><<<a.rows, 512, 0, stream>>>(a);
+  return launched();
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t fm_pages_work_ints(int32_t n_pages, int32_t max_seqs) {
+  if (n_pages < 1 || max_seqs < 1 || max_seqs > FM_MAX_SEQS) return 0;
+  fm_pages p{};
+  p.n_pages = n_pages; p.max_seqs = max_seqs;
+  return (size_t)pg::word_at(p) + 1;
+}
+
+int fm_pages_reset(const fm_pages* p, void* stream) {
+  const int rc = check_pages(p);
+  if (rc != FM_OK) return rc;
+  pg::reset_kernel<<<148, 256, 0, as_stream(stream)>>>(*p);
+  return launched();
+}
+
+int fm_pages_fork(const fm_pages* p, const int32_t* src, const int32_t* dst, int32_t n, void* stream) {
+  int rc = check_pages(p);
+  if (rc == FM_OK) rc = check_list(src, dst, n);
+  if (rc != FM_OK || n == 0) return rc;
+  pg::fork_kernel<<<n, 128, 0, as_stream(stream)>>>(*p, src, dst, n);
+  return launched();
+}
+
+int fm_pages_reserve(const fm_pages* p, const fm_cache* c, const int32_t* seqs, const int32_t* grow, int32_t n, void* stream) {
+  int rc = check_both(p, c);
+  if (rc == FM_OK) rc = check_list(seqs, grow, n);
+  if (rc == FM_OK && n > p->max_seqs) rc = FM_ERR_INVALID_ARG;       // (the jobs of the entries have a place each)
+  if (rc != FM_OK || n == 0) return rc;
+  pg::reserve_plan_kernel<<<1, pg::PLAN, 0, as_stream(stream)>>>(*p, seqs, grow, n);
+  if (cudaGetLastError() != cudaSuccess) return FM_ERR_CUDA;
+  return launch_behind(pg::reserve_copy_kernel, dim3(n, 2 * c->n_layers), 256, as_stream(stream), *p, geo_of(*c)) == cudaSuccess ? FM_OK : FM_ERR_CUDA;
+}
+
+int fm_pages_append(const fm_pages* p, const fm_cache* c, const fm_new_rows* rows, const int32_t* seqs, const int32_t* row_off, const int32_t* path,
+                    int32_t path_stride, const int32_t* n_acc, int32_t n, int32_t max_rows, void* stream) {
+  int rc = check_both(p, c);
+  if (rc == FM_OK) rc = check_list(seqs, row_off, n);
+  if (rc == FM_OK && n > p->max_seqs) rc = FM_ERR_INVALID_ARG;
+  if (rc != FM_OK) return rc;
+  if (rows == nullptr || rows->k == nullptr || rows->v == nullptr || !aligned16(rows->k) || !aligned16(rows->v) || max_rows < 0) return FM_ERR_INVALID_ARG;
+  if ((rows->layer_stride | rows->row_stride | rows->head_stride) & 7) return FM_ERR_INVALID_ARG;
+  if (path != nullptr && (n_acc == nullptr || path_stride < 1)) return FM_ERR_INVALID_ARG;
+  if (n == 0) return FM_OK;
+  pg::Rows r;
+  r.k = static_cast<const char*>(rows->k); r.v = static_cast<const char*>(rows->v);
+  r.layer = 2 * rows->layer_stride; r.row = 2 * rows->row_stride; r.head = 2 * rows->head_stride;
+  pg::append_kernel<<<dim3(n, 2 * c->n_layers), 256, 0, as_stream(stream)>>>(*p, geo_of(*c), r, seqs, row_off, path, path_stride, n_acc, max_rows);
+  return launched();
+}
+
+int fm_pages_truncate(const fm_pages* p, const int32_t* seqs, const int32_t* new_lens, int32_t n, void* stream) {
+  int rc = check_pages(p);
+  if (rc == FM_OK) rc = check_list(seqs, new_lens, n);
+  if (rc != FM_OK || n == 0) return rc;
+  pg::truncate_kernel<<<n, 128, 0, as_stream(stream)>>>(*p, seqs, new_lens);
+  return launched();
+}
+
+int fm_pages_compact(const fm_pages* p, const fm_cache* c, int32_t* used, void* stream) {
+  const int rc = check_both(p, c);
+  if (rc != FM_OK) return rc;
+  pg::compact_plan_kernel<<<1, pg::PLAN, 0, as_stream(stream)>>>(*p, used);
+  if (cudaGetLastError() != cudaSuccess) return FM_ERR_CUDA;
+  // enough blocks for every SM; no more than there can be pages to move
+  const int rows = 2 * c->n_layers + 1, most = p->n_pages / 2 + 1, want = (148 * 16 + rows - 1) / rows;
+  return launch_behind(pg::compact_copy_kernel, dim3(want < most ? want : most, rows), 256, as_stream(stream), *p, geo_of(*c)) == cudaSuccess ? FM_OK : FM_ERR_CUDA;
+}
+
+size_t fm_tree_attention_bytes(const fm_cache* cache, const fm_tree_args* args) {
+  if (check_tree(cache, args) != FM_OK) return 0;
+  return 4096 + part_bytes(16, cache->head_dim);
+}
+
+int fm_tree_attention(const fm_cache* c, int32_t layer, const fm_tree_args* t, void* workspace, size_t workspace_bytes, void* stream) {
+  const int rc = check_tree(c, t);
+  if (rc != FM_OK) return rc;
+  if (layer < 0 || layer >= c->n_layers || workspace == nullptr || (reinterpret_cast<uintptr_t>(workspace) & 255) != 0) return FM_ERR_INVALID_ARG;
+  if (workspace_bytes < fm_tree_attention_bytes(c, t)) return FM_ERR_CAPACITY;
+  tr::Args a{};
+  a.q = t->q; a.k_new = t->k_new; a.v_new = t->v_new; a.out = t->out; a.lse = t->lse;
+  a.q_row = t->q_row_stride; a.new_row = t->new_row_stride; a.out_row = t->out_row_stride;
+  a.k = static_cast<const char*>(c->k) + 2 * layer * c->layer_stride;
+  a.v = static_cast<const char*>(c->v) + 2 * layer * c->layer_stride;
+  a.page = c->page_stride; a.head = c->head_stride; a.slot = c->slot_stride;
+  a.table = t->table; a.lens = t->lens; a.seqs = t->seqs; a.row_off = t->row_off; a.parent = t->parent; a.status = t->status;
+  a.desc = static_cast<int4*>(workspace);
+  a.part = reinterpret_cast<float*>(static_cast<char*>(workspace) + 4096);
+  a.page_div = div_by(c->page_slots);
+  a.n_pages = c->n_pages; a.max_pages = t->max_pages; a.max_seqs = t->max_seqs; a.batch = t->batch;
+  a.H = t->n_heads; a.Hkv = c->n_kv_heads; a.G = t->n_heads / c->n_kv_heads; a.max_nodes = t->max_nodes;
+  const int64_t holds = (int64_t)t->max_pages * c->page_slots;
+  a.max_len = t->max_len < holds ? t->max_len : (int)holds;
+  a.window = t->window; a.n_prefix = t->n_prefix;
+  a.scale_log2 = t->scale * 1.4426950408889634f;
+  if (c->dtype == FM_BF16) return c->head_dim == 64 ? tree_rows16<bf16, 64>(a, as_stream(stream)) : tree_rows16<bf16, 128>(a, as_stream(stream));
+  return c->head_dim == 64 ? tree_rows16<__half, 64>(a, as_stream(stream)) : tree_rows16<__half, 128>(a, as_stream(stream));
+}
+
+int fm_tree_accept(const int32_t* tokens, const int32_t* parent, const int32_t* row_off, const int32_t* predicted, int32_t batch, int32_t* path,
+                   int32_t path_stride, int32_t* n_acc, int32_t* next_tok, void* stream) {
+  if (tokens == nullptr || parent == nullptr || row_off == nullptr || predicted == nullptr || path == nullptr || n_acc == nullptr || next_tok == nullptr)
+    return FM_ERR_INVALID_ARG;
+  if (batch < 1 || path_stride < 1) return FM_ERR_INVALID_ARG;
+  tr::accept_kernel<<<(batch + 3) / 4, 128, 0, as_stream(stream)>>>(tokens, parent, row_off, predicted, batch, path, path_stride, n_acc, next_tok);
+  return launched();
+}
+
+int fm_logprobs(const void* logits, int32_t dtype, int32_t rows, int32_t vocab, int64_t row_stride, const int32_t* tokens, float* logprob, float* entropy,
+                int32_t* rank, int32_t top, int32_t* top_ids, float* top_logprobs, void* stream) {
+  if (logits == nullptr || rows < 0 || vocab < 1 || row_stride < vocab || top < 0 || top > vocab) return FM_ERR_INVALID_ARG;
+  if (dtype != FM_BF16 && dtype != FM_FP16 && dtype != FM_FP32) return FM_ERR_INVALID_ARG;
+  if ((reinterpret_cast<uintptr_t>(logits) & (dtype == FM_FP32 ? 3 : 1)) != 0) return FM_ERR_INVALID_ARG;
+  if (top > FM_MAX_TOP) return FM_ERR_CAPACITY;
+  if (rows == 0) return FM_OK;
+  lp::Args a{logits, tokens, logprob, entropy, rank, top_ids, top_logprobs, row_stride, rows, vocab, top_ids == nullptr && top_logprobs == nullptr ? 0 : top};
+  if (dtype == FM_FP32) return score_rows<float>(a, as_stream(stream));
+  if (dtype == FM_BF16) return score_rows<bf16>(a, as_stream(stream));
+  return score_rows<__half>(a, as_stream(stream));
+}
+
+}  // extern "C"
