@@ -423,7 +423,8 @@ int fm_device_status(fm_ctx* ctx);
 
 #define FM_MAX_TOP 32               /* alternatives per row of fm_logprobs                          */
 #define FM_MAX_TREE_NODES 256       /* nodes of one tree                                            */
-#define FM_MAX_SEQS 4096            /* sequences of one fm_pages, entries of one call               */
+#define FM_MAX_SEQS 4096            /* sequences of one fm_pages, entries of one of its calls       */
+#define FM_MAX_TREES 1024           /* trees of one fm_tree_attention                               */
 
 /* A pool of cache pages: element i of the key of position `slot` of page `page`, head h, layer l is
  * k[l*layer_stride + page*page_stride + h*head_stride + slot*slot_stride + i]; values alike.  Strides
@@ -506,7 +507,7 @@ int fm_pages_compact(const fm_pages* pages, const fm_cache* cache, int32_t* used
  * effect on it, whatever they hold.  Rows behind row_off[n] are left as they were.  Nodes behind max_nodes, and
  * positions behind the table or max_len, are not seen; rows of such nodes are left as they were.
  * Nothing is appended to the cache.  Errors: INVALID_ARG (null pointer, size, stride or alignment),
- * UNSUPPORTED (head_dim not 64 / 128, dtype), CAPACITY (workspace, batch > FM_MAX_SEQS, max_nodes > FM_MAX_TREE_NODES). */
+ * UNSUPPORTED (head_dim not 64 / 128, dtype), CAPACITY (workspace, batch > FM_MAX_TREES, max_nodes > FM_MAX_TREE_NODES). */
 typedef struct fm_tree_args {
   const void* q;                    /* DEV [rows, n_heads, head_dim], rows q_row_stride apart        */
   const void* k_new; const void* v_new;   /* DEV [rows, n_kv_heads, head_dim], rows new_row_stride apart */
@@ -520,7 +521,7 @@ typedef struct fm_tree_args {
   const int32_t* parent;            /* DEV [rows]                                                    */
   int32_t* status;                  /* DEV [1] or NULL: TIMEOUT if a bounded wait gave up            */
   int32_t max_pages, max_seqs, batch, n_heads, max_nodes, max_len, window, n_prefix;
-  float scale;
+  float scale;                      /* above 0                                                       */
 } fm_tree_args;
 size_t fm_tree_attention_bytes(const fm_cache* cache, const fm_tree_args* args);   /* workspace; 0 if the arguments are invalid */
 int fm_tree_attention(const fm_cache* cache, int32_t layer, const fm_tree_args* args, void* workspace /*DEV, 256-byte aligned*/,

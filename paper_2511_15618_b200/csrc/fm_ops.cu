@@ -2,6 +2,7 @@
 // The host checks the arguments, picks a kernel by sizes and types and enqueues it.
 #include "../../include/flashmesh.h"
 
+#include <cuda.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
 
@@ -106,30 +107,103 @@ int check_tree(const fm_cache* c, const fm_tree_args* t) {
   if ((t->q_row_stride | t->new_row_stride | t->out_row_stride) & 7) return FM_ERR_INVALID_ARG;
   if (t->q_row_stride < (int64_t)t->n_heads * c->head_dim || t->out_row_stride < (int64_t)t->n_heads * c->head_dim ||
       t->new_row_stride < (int64_t)c->n_kv_heads * c->head_dim) return FM_ERR_INVALID_ARG;
-  if (!(t->scale == t->scale) || t->scale - t->scale != 0.f) return FM_ERR_INVALID_ARG;
+  if (!(t->scale > 0.f) || t->scale - t->scale != 0.f) return FM_ERR_INVALID_ARG;
   if (c->head_dim != 64 && c->head_dim != 128) return FM_ERR_UNSUPPORTED;
-  if (t->batch > FM_MAX_SEQS || t->max_nodes > FM_MAX_TREE_NODES || (int64_t)t->max_pages * c->page_slots > MOST_SLOTS) return FM_ERR_CAPACITY;
+  if (t->batch > FM_MAX_TREES || t->max_nodes > FM_MAX_TREE_NODES || (int64_t)t->max_pages * c->page_slots > MOST_SLOTS) return FM_ERR_CAPACITY;
   return FM_OK;
 }
 
-constexpr size_t DESC_BYTES = 16 * tr::CTAS + 128;
-static_assert(DESC_BYTES % 256 == 0 || DESC_BYTES < 4096, "");
-inline size_t part_bytes(int rows, int dh) { return (size_t)tr::CTAS * 2 * rows * (dh + 2) * sizeof(float); }
-
-template <typename T, int DH>
-int tree_rows16(const tr::Args& a, cudaStream_t stream) {
-  static std::atomic<uint64_t> asked{0};
-  using CF = tr::Rows16<DH>;
-  if (!allow_smem(tr::rows16_kernel<T, DH>, CF::bytes(FM_MAX_SEQS), asked)) return FM_ERR_CUDA;
-  tr::rows16_kernel<T, DH><<<tr::CTAS, CF::THREADS, CF::bytes(a.batch), stream>>>(a);
-  if (cudaGetLastError() != cudaSuccess) return FM_ERR_CUDA;
-  return launch_behind(tr::merge_kernel<T, DH, 16>, dim3(tr::CTAS, 4), 256, stream, a) == cudaSuccess ? FM_OK : FM_ERR_CUDA;
+// Rows that share keys (nodes x heads of a group): up to 16 take the warp-level form, more the tensor cores' tiles of 128.
+inline bool few_rows(int max_nodes, int group) { return (int64_t)max_nodes * group <= 16; }
+constexpr size_t DESC_BYTES = 8192;                          // of up to 2 * 148 CTAs
+static_assert(DESC_BYTES >= 2 * tr::SMS * sizeof(int4), "");
+static_assert(tr::Rows16<128>::C == tr::Rows128<64>::C && tr::Rows16<128>::C == tr::Rows128<128>::C, "make_maps: one chunk for the three of them");
+static_assert(tr::Rows16<128>::FIXED + tr::plan_bytes(FM_MAX_TREES) <= 227 * 1024 && tr::Rows128<128>::FIXED + tr::plan_bytes(FM_MAX_TREES) <= 227 * 1024, "");
+inline size_t tree_bytes(bool few, int dh) {
+  return DESC_BYTES + (size_t)(few ? tr::SMS : 2 * tr::SMS) * 2 * (few ? 16 : 128) * (dh + 2) * sizeof(float);
 }
 
+typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                                  const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+EncodeTiledFn encode_tiled_fn() {
+  static const EncodeTiledFn fn = [] {
+    void* p = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    const bool ok = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) == cudaSuccess && q == cudaDriverEntryPointSuccess;
+    return ok ? reinterpret_cast<EncodeTiledFn>(p) : nullptr;
+  }();
+  return fn;
+}
+// A layer's pool as (features, slots, heads, pages), boxes of 64 features and min(page, chunk) slots, 128-byte swizzle.
+// Boxes have to fill a chunk evenly and start where the swizzle does (8 rows); other page sizes, and strides that a map
+// cannot hold, are copied by threads.
+bool make_maps(const fm_cache& c, int layer, int chunk, tr::Args& a) {
+  const int ps = c.page_slots;
+  if (ps % 8 != 0 || (chunk % ps != 0 && ps % chunk != 0)) return false;
+  const EncodeTiledFn fn = encode_tiled_fn();
+  if (fn == nullptr) return false;
+  const int64_t most = (int64_t)1 << 39;
+  for (int64_t s : {c.slot_stride, c.head_stride, c.page_stride})
+    if (s <= 0 || s >= most) return false;
+  const cuuint64_t dim[4] = {(cuuint64_t)c.head_dim, (cuuint64_t)ps, (cuuint64_t)c.n_kv_heads, (cuuint64_t)c.n_pages};
+  const cuuint64_t stride[3] = {(cuuint64_t)c.slot_stride * 2, (cuuint64_t)c.head_stride * 2, (cuuint64_t)c.page_stride * 2};
+  const cuuint32_t box[4] = {64, (cuuint32_t)(ps < chunk ? ps : chunk), 1, 1}, one[4] = {1, 1, 1, 1};
+  const CUtensorMapDataType type = c.dtype == FM_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
+  for (int kv = 0; kv < 2; ++kv) {
+    char* base = static_cast<char*>(kv == 0 ? c.k : c.v) + 2 * layer * c.layer_stride;
+    if (fn(kv == 0 ? &a.map_k : &a.map_v, type, 4, base, dim, stride, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+           CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+      return false;
+  }
+  return true;
+}
+
+template <typename T, int DH>
+int tree_attention(const tr::Args& a, cudaStream_t stream) {
+  cudaError_t e;
+  if (few_rows(a.max_nodes, a.G)) {
+    static std::atomic<uint64_t> asked{0};
+    using CF = tr::Rows16<DH>;
+    if (!allow_smem(tr::rows16_kernel<T, DH>, CF::bytes(FM_MAX_TREES), asked)) return FM_ERR_CUDA;
+    tr::rows16_kernel<T, DH><<<tr::SMS, CF::THREADS, CF::bytes(a.batch), stream>>>(a);
+    if (cudaGetLastError() != cudaSuccess) return FM_ERR_CUDA;
+    e = launch_behind(tr::merge_kernel<T, DH, 16>, dim3(tr::SMS, 4), 256, stream, a);
+  } else {
+    static std::atomic<uint64_t> asked{0};
+    using CF = tr::Rows128<DH>;
+    if (!allow_smem(tr::rows128_kernel<T, DH>, CF::bytes(FM_MAX_TREES), asked)) return FM_ERR_CUDA;
+    tr::rows128_kernel<T, DH><<<2 * tr::SMS, CF::THREADS, CF::bytes(a.batch), stream>>>(a);
+    if (cudaGetLastError() != cudaSuccess) return FM_ERR_CUDA;
+    e = launch_behind(tr::merge_kernel<T, DH, 128>, dim3(2 * tr::SMS, 8), 256, stream, a);
+  }
+  return e == cudaSuccess ? FM_OK : FM_ERR_CUDA;
+}
+
+template <typename T, int R>
+int score_short(const lp::Args& a, cudaStream_t stream) {
+  lp::short_kernel<T, R><<<(a.rows + lp::SHORT_WARPS - 1) / lp::SHORT_WARPS, 32 * lp::SHORT_WARPS, 0, stream>>>(a);
+  return launched();
+}
+
+// Rows whose vectors fit into a warp's registers (64 values a lane) take a warp, longer ones a block: of 256 threads, or of 512
+// where there are too few rows to fill the SMs with the smaller one.
 template <typename T>
 int score_rows(const lp::Args& a, cudaStream_t stream) {
-  if (a.vocab <= 2048) lp::rows_kernel<T, 128><<<a.rows, 128, 0, stream>>>(a);
-  else lp::rows_kernel<T, 512><<<a.rows, 512, 0, stream>>>(a);
+  constexpr int N = lp::Vec<T>::N, MOST = 64 / N;
+  const int vectors = (a.vocab / N + 31) / 32;               // a lane
+  if (vectors <= MOST) {
+    if (vectors <= 1) return score_short<T, 1>(a, stream);
+    if (vectors <= MOST / 4) return score_short<T, MOST / 4>(a, stream);
+    if (vectors <= MOST / 2) return score_short<T, MOST / 2>(a, stream);
+    return score_short<T, MOST>(a, stream);
+  }
+  if (a.rows >= 2 * 148) {
+    lp::long_kernel<T, 256, 8><<<a.rows, 256, 8 * 256 * 16, stream>>>(a);
+  } else {
+    static std::atomic<uint64_t> asked{0};
+    if (!allow_smem(lp::long_kernel<T, 512, 8>, 8 * 512 * 16, asked)) return FM_ERR_CUDA;
+    lp::long_kernel<T, 512, 8><<<a.rows, 512, 8 * 512 * 16, stream>>>(a);
+  }
   return launched();
 }
 
@@ -206,7 +280,7 @@ int fm_pages_compact(const fm_pages* p, const fm_cache* c, int32_t* used, void* 
 
 size_t fm_tree_attention_bytes(const fm_cache* cache, const fm_tree_args* args) {
   if (check_tree(cache, args) != FM_OK) return 0;
-  return 4096 + part_bytes(16, cache->head_dim);
+  return tree_bytes(few_rows(args->max_nodes, args->n_heads / cache->n_kv_heads), cache->head_dim);
 }
 
 int fm_tree_attention(const fm_cache* c, int32_t layer, const fm_tree_args* t, void* workspace, size_t workspace_bytes, void* stream) {
@@ -222,7 +296,7 @@ int fm_tree_attention(const fm_cache* c, int32_t layer, const fm_tree_args* t, v
   a.page = c->page_stride; a.head = c->head_stride; a.slot = c->slot_stride;
   a.table = t->table; a.lens = t->lens; a.seqs = t->seqs; a.row_off = t->row_off; a.parent = t->parent; a.status = t->status;
   a.desc = static_cast<int4*>(workspace);
-  a.part = reinterpret_cast<float*>(static_cast<char*>(workspace) + 4096);
+  a.part = reinterpret_cast<float*>(static_cast<char*>(workspace) + DESC_BYTES);
   a.page_div = div_by(c->page_slots);
   a.n_pages = c->n_pages; a.max_pages = t->max_pages; a.max_seqs = t->max_seqs; a.batch = t->batch;
   a.H = t->n_heads; a.Hkv = c->n_kv_heads; a.G = t->n_heads / c->n_kv_heads; a.max_nodes = t->max_nodes;
@@ -230,8 +304,10 @@ int fm_tree_attention(const fm_cache* c, int32_t layer, const fm_tree_args* t, v
   a.max_len = t->max_len < holds ? t->max_len : (int)holds;
   a.window = t->window; a.n_prefix = t->n_prefix;
   a.scale_log2 = t->scale * 1.4426950408889634f;
-  if (c->dtype == FM_BF16) return c->head_dim == 64 ? tree_rows16<bf16, 64>(a, as_stream(stream)) : tree_rows16<bf16, 128>(a, as_stream(stream));
-  return c->head_dim == 64 ? tree_rows16<__half, 64>(a, as_stream(stream)) : tree_rows16<__half, 128>(a, as_stream(stream));
+  const bool few = few_rows(a.max_nodes, a.G);
+  a.tma = make_maps(*c, layer, few && c->head_dim == 64 ? tr::Rows16<64>::C : tr::Rows16<128>::C, a) ? 1 : 0;
+  if (c->dtype == FM_BF16) return c->head_dim == 64 ? tree_attention<bf16, 64>(a, as_stream(stream)) : tree_attention<bf16, 128>(a, as_stream(stream));
+  return c->head_dim == 64 ? tree_attention<__half, 64>(a, as_stream(stream)) : tree_attention<__half, 128>(a, as_stream(stream));
 }
 
 int fm_tree_accept(const int32_t* tokens, const int32_t* parent, const int32_t* row_off, const int32_t* predicted, int32_t batch, int32_t* path,

@@ -1,14 +1,13 @@
 // Attention of trees of drafted tokens over a paged cache, and the walk that accepts a path.
 //
-// A tile is what shares keys: the query rows (nodes x heads of the group) of one sequence and kv-head, 16 of them.  Its keys
-// come in chunks of C: conditioning slots, the window's slots (or all cached ones), the nodes.  The launch is one CTA per
-// SM whatever the lengths: the chunks of all tiles, one tile after the other, are cut into equal shares (their total is
+// A tile is what shares keys: the query rows (nodes x heads of the group) of one sequence and kv-head, 16 or 128 of them.  Its keys
+// come in chunks of C: conditioning slots, the window's slots (or all cached ones), the nodes.  The launch is one or two CTAs
+// per SM whatever the lengths: the chunks of all tiles, one tile after the other, are cut into equal shares (their total is
 // known on the device alone), so ragged batches are balanced without the host.  A cut falls inside a tile at most once per CTA; the
 // parts of a cut tile go to a scratch buffer and a second small launch merges them in order.
-// Loading: four warps copy 16 bytes a thread straight into swizzled shared memory (cp.async: page, head and slot strides
-// are free, what is not there is filled with zeros), a ring of stages ahead of the four warps that multiply; page ids are
-// fetched a chunk ahead.  The multiplying warps each own a slice of every chunk and their own running maximum, sum
-// and output (base 2), merged at the end of a tile.
+// Loading: a page's slots (or a chunk's, where pages are larger) of a head are one TMA box, swizzled for the multiplication; one warp
+// requests chunks ahead of the warps that multiply, through a ring of stages.  Page sizes whose boxes do not fill a chunk
+// evenly, and the nodes' rows, are copied 16 bytes a thread (cp.async) into the same layout.
 // Ancestors: reach[i], a bit per node, by pointer doubling over the parents (log2 of the depth rounds).
 // Values a row does not see have no effect on it: scores are replaced by -inf; values that are not finite in chunks
 // where some row does not see all keys are taken out of the product and added to the rows that do see them.
@@ -16,12 +15,13 @@
 #include <cuda_fp16.h>
 
 #include "fm_common.cuh"
+#include "fm_gemm_tc.cuh"
 #include "fm_ptx.cuh"
 #include "../../include/flashmesh.h"
 
 namespace tr {
 
-constexpr int CTAS = 148;               // a B200 has as many SMs; the workspace is laid out for them
+constexpr int SMS = 148;                // of a B200: one CTA each (16-row tiles) or two (128); the workspace is laid out for them
 constexpr int WORDS = FM_MAX_TREE_NODES / 32;
 
 struct Div {                            // division of 0 <= n < 2^31 by a constant
@@ -38,11 +38,13 @@ struct Args {
   int64_t page, head, slot;             // elements
   const int *table, *lens, *seqs, *row_off, *parent;
   int* status;
-  float* part;                          // [CTAS * 2][ROWS][DH + 2]
-  int4* desc;                           // [CTAS]: sequence, kv-head, tile, parts of the tile that starts here and is cut
+  float* part;                          // [CTAs * 2][ROWS][DH + 2]
+  int4* desc;                           // [CTAs]: sequence, kv-head, tile, parts of the tile that starts here and is cut
   Div page_div;
   int n_pages, max_pages, max_seqs, batch, H, Hkv, G, max_nodes, max_len, window, n_prefix;
   float scale_log2;
+  int tma;                              // the page size suits the boxes
+  alignas(64) CUtensorMap map_k, map_v; // the layer's pool as [pages][heads][slots][head_dim], box 64 features x min(page, C) slots
 };
 
 // ---- element types
@@ -83,21 +85,23 @@ __device__ inline void cp_arrive(uint64_t* bar) {            // when this thread
 
 // ---- what a sequence asks for
 struct Seq {
-  int r0, n, len, pre, lo, seq;         // first row, nodes, cached positions; slots [0, pre) and [lo, len) are seen by some row
+  int r0, n, len, seq;                  // first row, nodes, cached positions, its row of the table
+  int pre, lo;                          // slots [0, pre) and [lo, len) are loaded; both ranges start at a multiple of C
   int n_pre, n_main, chunks, tiles;     // chunks of the two ranges, all chunks, query tiles per kv-head
 };
+__device__ inline int4 read_sequence(const Args& a, int b) {                   // (r0, n, len, seq) from the caller's arrays
+  const int r0 = a.row_off[b], n = a.row_off[b + 1] - r0, seq = a.seqs != nullptr ? a.seqs[b] : b;
+  const int len = seq >= 0 && seq < a.max_seqs ? max(0, min(a.lens[seq], a.max_len)) : 0;
+  return make_int4(r0, r0 < 0 || n < 0 ? 0 : min(n, a.max_nodes), len, seq);
+}
 template <int C, int ROWS>
-__device__ inline Seq sequence(const Args& a, int b) {
+__device__ inline Seq sequence(const Args& a, int4 v) {
   Seq s;
-  s.r0 = a.row_off[b];
-  s.n = a.row_off[b + 1] - s.r0;
-  s.n = s.r0 < 0 || s.n < 0 ? 0 : min(s.n, a.max_nodes);
-  s.seq = a.seqs != nullptr ? a.seqs[b] : b;
-  s.len = s.seq >= 0 && s.seq < a.max_seqs ? max(0, min(a.lens[s.seq], a.max_len)) : 0;
+  s.r0 = v.x; s.n = v.y; s.len = v.z; s.seq = v.w;
   s.pre = min(a.n_prefix, s.len);
-  s.lo = a.window > 0 ? max(s.pre, s.len - a.window + 1) : s.pre;
-  s.lo = min(s.lo, s.len);
-  if (s.lo == s.pre) { s.pre = 0; s.lo = 0; }                // one range
+  s.lo = a.window > 0 ? max(s.pre, s.len - a.window + 1) : 0;
+  s.lo = min(s.lo, s.len) / C * C;
+  if (s.lo < (s.pre + C - 1) / C * C) { s.pre = 0; s.lo = 0; }                 // one range
   s.n_pre = (s.pre + C - 1) / C;
   s.n_main = (s.len - s.lo + C - 1) / C;
   s.chunks = s.n_pre + s.n_main + (s.n + C - 1) / C;
@@ -105,16 +109,17 @@ __device__ inline Seq sequence(const Args& a, int b) {
   return s;
 }
 
-// ---- the cut of all chunks into shares
+// ---- the cut of all chunks into shares.  A tile counts OVER chunks more than it has: what starting and ending it takes.
+constexpr int OVER = 2;
 struct Plan {
-  const long long* base;                // [batch + 1] chunks in front of a sequence's
+  const long long* base;                // [batch + 1] units in front of a sequence's
   const int* tile_base;                 // [batch + 1] tiles in front of a sequence's
+  const int4* info;                     // [batch]
   int batch;
   long long total, share;
   bool whole;                           // CTA i takes tile i: nothing is cut
 };
-struct Place { int b; long long tile; int off; };            // sequence, tile of the sequence (kv-head * tiles + tile), chunk
-// last sequence whose first chunk (tile) is not behind x, and that has any
+// last sequence whose first unit (tile) is not behind x, and that has any
 template <typename V>
 __device__ inline int find(const V* base, int batch, long long x) {
   int lo = 0, hi = batch;                                    // base[lo] <= x < base[hi]
@@ -124,25 +129,24 @@ __device__ inline int find(const V* base, int batch, long long x) {
   }
   return lo;
 }
-// first chunk of CTA i's share.  A cut close to the border of a tile moves there: the tile stays whole.
+// first unit of CTA i's share.  A cut close to the border of a tile moves there: the tile stays whole.
 template <int C, int ROWS>
 __device__ inline long long boundary(const Args& a, const Plan& p, int i) {
   const long long x = p.share * i;
   if (i <= 0) return 0;
   if (x >= p.total) return p.total;
-  const int b = find(p.base, p.batch, x);
-  const Seq s = sequence<C, ROWS>(a, b);
-  const int off = (int)((x - p.base[b]) % s.chunks);
+  const int b = find(p.base, p.batch, x), units = sequence<C, ROWS>(a, p.info[b]).chunks + OVER;
+  const int off = (int)((x - p.base[b]) % units);
   const long long near = p.share >> 3;
-  if (off <= near) return x - off;
-  if (s.chunks - off <= near) return x - off + s.chunks;
+  if (off <= near + OVER) return x - off;
+  if (units - off <= near) return x - off + units;
   return x;
 }
 
 // walks over the chunks of a CTA
 template <int C, int ROWS>
 struct Walk {
-  long long at, end;                    // next chunk, end of the share
+  long long at, end;                    // next unit, end of the share
   Seq s;
   int b, tile, c, c_end;                // tile of the sequence; next chunk of it, end of the share's part
   long long tile_start;
@@ -150,14 +154,14 @@ struct Walk {
     if (p.whole) {
       const bool any = cta < p.tile_base[p.batch];
       b = any ? find(p.tile_base, p.batch, cta) : 0;
-      s = sequence<C, ROWS>(a, b);
-      at = any ? p.base[b] + (long long)(cta - p.tile_base[b]) * s.chunks : 0;
-      end = any ? at + s.chunks : 0;
+      s = sequence<C, ROWS>(a, p.info[b]);
+      at = any ? p.base[b] + (long long)(cta - p.tile_base[b]) * (s.chunks + OVER) : 0;
+      end = any ? at + s.chunks + OVER : 0;
     } else {
       at = boundary<C, ROWS>(a, p, cta);
       end = boundary<C, ROWS>(a, p, cta + 1);
       b = at < end ? find(p.base, p.batch, at) : 0;
-      s = sequence<C, ROWS>(a, b);
+      s = sequence<C, ROWS>(a, p.info[b]);
     }
   }
   // the next tile, or part of one
@@ -165,16 +169,18 @@ struct Walk {
     if (at >= end) return false;
     if (at >= p.base[b + 1]) {
       do ++b; while (p.base[b + 1] == p.base[b]);
-      s = sequence<C, ROWS>(a, b);
+      s = sequence<C, ROWS>(a, p.info[b]);
     }
-    const long long in = at - p.base[b];
-    tile = (int)(in / s.chunks);
-    tile_start = p.base[b] + (long long)tile * s.chunks;
-    c = (int)(at - tile_start);
-    c_end = (int)(end - tile_start < s.chunks ? end - tile_start : s.chunks);
-    at = tile_start + c_end;
+    const int units = s.chunks + OVER;
+    tile = (int)((at - p.base[b]) / units);
+    tile_start = p.base[b] + (long long)tile * units;
+    c = max(0, (int)(at - tile_start) - OVER);               // (cuts lie behind the first OVER units or in front of them)
+    c_end = (int)(end - tile_start < units ? end - tile_start : units) - OVER;
+    at = tile_start + OVER + c_end;
     return true;
   }
+  __device__ bool starts() const { return c == 0; }
+  __device__ bool ends() const { return c_end == s.chunks; }
 };
 
 // a chunk: keys [start, start + n) of the cache, or nodes
@@ -191,7 +197,7 @@ __device__ inline Chunk chunk_of(const Seq& s, int c) {
 
 // ---- prefix sums over the sequences, by a block of THREADS
 template <int C, int ROWS, int THREADS>
-__device__ inline void make_plan(const Args& a, Plan& p, long long* base, int* tile_base, long long* sh) {
+__device__ inline void make_plan(const Args& a, Plan& p, int4* info, long long* base, int* tile_base, long long* sh) {
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
   long long carry = 0;
   int t_carry = 0, longest = 0;
@@ -200,9 +206,11 @@ __device__ inline void make_plan(const Args& a, Plan& p, long long* base, int* t
     long long units = 0;
     int tiles = 0;
     if (b < a.batch) {
-      const Seq s = sequence<C, ROWS>(a, b);
+      const int4 v = read_sequence(a, b);
+      info[b] = v;
+      const Seq s = sequence<C, ROWS>(a, v);
       tiles = s.tiles * a.Hkv;
-      units = (long long)tiles * s.chunks;
+      units = (long long)tiles * (s.chunks + OVER);
       if (tiles > 0) longest = max(longest, s.chunks);
     }
     long long x = units;
@@ -218,7 +226,7 @@ __device__ inline void make_plan(const Args& a, Plan& p, long long* base, int* t
     __syncthreads();
     long long bx = carry;
     int bt = t_carry;
-    for (int k = 0; k < THREADS / 32; ++k) {
+    for (int k = 0; k < (THREADS + 31) / 32; ++k) {
       if (k < w) { bx += sh[2 * k]; bt += (int)sh[2 * k + 1]; }
       carry += sh[2 * k];
       t_carry += (int)sh[2 * k + 1];
@@ -231,14 +239,15 @@ __device__ inline void make_plan(const Args& a, Plan& p, long long* base, int* t
   if (threadIdx.x == 0) { base[a.batch] = carry; tile_base[a.batch] = t_carry; }
   __syncthreads();
   for (int k = 0; k < THREADS / 32; ++k) longest = max(longest, (int)sh[k]);
-  p.base = base; p.tile_base = tile_base; p.batch = a.batch;
+  p.base = base; p.tile_base = tile_base; p.info = info; p.batch = a.batch;
   p.total = carry;
   p.share = (carry + gridDim.x - 1) / gridDim.x;
-  if (p.share < 1) p.share = 1;
-  // Few tiles that are short, or all alike: a CTA each.  (Cutting a tile of up to six chunks costs more in parts than it gains.)
-  const long long most = p.share + (p.share >> 2) > 6 ? p.share + (p.share >> 2) : 6;
+  if (p.share <= 2 * OVER) p.share = 2 * OVER + 1;           // (a cut inside a tile then leaves chunks on both sides)
+  // Few tiles that are short, or all alike: a CTA each.  (Cutting a tile of up to eight chunks costs more in parts than it gains.)
+  const long long most = p.share + (p.share >> 2) > 8 ? p.share + (p.share >> 2) : 8;
   p.whole = t_carry <= (int)gridDim.x && longest <= most;
 }
+__host__ __device__ constexpr int plan_bytes(int batch) { return 16 * batch + 12 * (batch + 1) + 24; }
 
 // CTA `cta` starts a tile that it does not end: how many CTAs share it
 template <int C, int ROWS>
@@ -246,6 +255,92 @@ __device__ inline int parts_of(const Args& a, const Plan& p, int cta, long long 
   int n = 1;
   while (cta + n < (int)gridDim.x && boundary<C, ROWS>(a, p, cta + n) < tile_end) ++n;
   return n;
+}
+
+// ---- loading, by a warp
+// a chunk of cached positions as TMA boxes; every lane arrives on the barrier once
+template <typename T, int DH, int C>
+__device__ inline void request_boxes(const Args& a, const Seq& s, const Chunk& k, int hk, unsigned char* Ks, unsigned char* Vs, uint64_t* bar, int lane) {
+  constexpr int HALVES = DH / 64;
+  const int rows = min(a.page_div.d, C), boxes = (k.n + rows - 1) / rows;      // (at most C / 8 = 16)
+  int id = -1, in_page = 0;
+  if (lane < boxes) {
+    const int slot = k.start + lane * rows, pi = a.page_div(slot);
+    id = __ldg(a.table + (int64_t)s.seq * a.max_pages + pi);
+    in_page = slot - pi * a.page_div.d;
+  }
+  const bool ok = id >= 0 && id < a.n_pages;
+  if (lane < boxes && !ok) {                                 // no page: zeros, and the caller is told
+    if (a.status != nullptr) atomicMin(a.status, FM_ERR_INVALID_ARG);
+    for (int h = 0; h < HALVES; ++h)
+      for (int i = 0; i < rows * 8; ++i) {
+        reinterpret_cast<uint4*>(Ks + (h * C + lane * rows) * 128)[i] = make_uint4(0u, 0u, 0u, 0u);
+        reinterpret_cast<uint4*>(Vs + (h * C + lane * rows) * 128)[i] = make_uint4(0u, 0u, 0u, 0u);
+      }
+    ptx::fence_proxy_async();
+  }
+  const int n = __popc(__ballot_sync(0xffffffffu, ok));
+  if (lane == 0) ptx::mbar_expect_tx(bar, (uint32_t)(n * rows * 128 * 2 * HALVES)); else ptx::mbar_arrive(bar);
+  __syncwarp();
+  if (ok) {
+#pragma unroll
+    for (int h = 0; h < HALVES; ++h) {
+      ptx::tma_load_4d(Ks + (h * C + lane * rows) * 128, &a.map_k, h * 64, in_page, hk, id, bar);
+      ptx::tma_load_4d(Vs + (h * C + lane * rows) * 128, &a.map_v, h * 64, in_page, hk, id, bar);
+    }
+  }
+  __syncwarp();
+}
+// the same with 16-byte copies, also for nodes; what is not there is zero.  The copies are the calling threads' (cp.async).
+template <typename T, int DH, int C>
+__device__ inline void request_pieces(const Args& a, const Seq& s, const Chunk& k, int hk, unsigned char* Ks, unsigned char* Vs, int lane) {
+  constexpr int PIECES = DH / 8, STEP = 32 / PIECES;
+  const int piece = lane % PIECES;
+  const uint32_t ks = ptx::smem_u32(Ks) + (piece >> 3) * C * 128, vs = ptx::smem_u32(Vs) + (piece >> 3) * C * 128;
+  const int* table = a.table + (int64_t)s.seq * a.max_pages;
+#pragma unroll 4
+  for (int r = lane / PIECES; r < C; r += STEP) {
+    bool there = r < k.n;
+    const T *kp = reinterpret_cast<const T*>(a.k), *vp = reinterpret_cast<const T*>(a.v);
+    int64_t at = 0;
+    if (k.tree) {
+      kp = static_cast<const T*>(a.k_new); vp = static_cast<const T*>(a.v_new);
+      if (there) at = (int64_t)(s.r0 + k.start + r) * a.new_row + hk * DH;
+    } else if (there) {
+      const int slot = k.start + r, pi = a.page_div(slot), id = __ldg(table + pi);
+      if (id < 0 || id >= a.n_pages) {
+        there = false;
+        if (a.status != nullptr) atomicMin(a.status, FM_ERR_INVALID_ARG);
+      } else {
+        at = id * a.page + hk * a.head + (int64_t)(slot - pi * a.page_div.d) * a.slot;
+      }
+    }
+    const uint32_t to = ptx::swz128(r, piece & 7);
+    cp16(ks + to, kp + at + piece * 8, there);
+    cp16(vs + to, vp + at + piece * 8, there);
+  }
+}
+// query rows of a tile, behind the last one zeros; halves of ROWS x 128 bytes
+template <typename T, int DH, int ROWS>
+__device__ inline void request_queries(const Args& a, const Seq& s, int hk, int mt, unsigned char* Q, int lane) {
+  constexpr int PIECES = DH / 8, STEP = 32 / PIECES;
+  const int piece = lane % PIECES, M = s.n * a.G;
+  const uint32_t qs = ptx::smem_u32(Q) + (piece >> 3) * ROWS * 128;
+#pragma unroll 4
+  for (int r = lane / PIECES; r < ROWS; r += STEP) {
+    const int idx = mt * ROWS + r;
+    const bool there = idx < M;
+    const int node = there ? idx / a.G : 0, gh = there ? idx - node * a.G : 0;
+    cp16(qs + ptx::swz128(r, piece & 7), static_cast<const T*>(a.q) + (int64_t)(s.r0 + node) * a.q_row + (hk * a.G + gh) * DH + piece * 8, there);
+  }
+}
+// after the last request: who else has parts of the tile that this CTA starts and does not end
+template <int C, int ROWS>
+__device__ inline void write_desc(const Args& a, const Plan& p, int4 cut, long long cut_end, int lane) {
+  if (lane == 0) {
+    if (cut.w != 0) cut.w = parts_of<C, ROWS>(a, p, blockIdx.x, cut_end);
+    a.desc[blockIdx.x] = cut;
+  }
 }
 
 // ---- ancestors of the nodes of a sequence, by `threads` threads that meet at `bar`: reach[i] (zero: not in use), depth[i]
@@ -316,138 +411,110 @@ __device__ inline void build_tree(Tree& t, const int* parent, int n, int tid, Sy
 // ------------------------------------------------------------------------------------------
 // sixteen query rows a tile, warp-level MMAs
 // ------------------------------------------------------------------------------------------
+// Eight warps multiply: four take the even chunks, four the odd ones, each a fixed slice of a chunk with its own running maximum,
+// sum and output (base 2); their states are merged at the end of a tile.  One warp loads, queries of the next tile included.
 template <int DH>
 struct Rows16 {
   static constexpr int ROWS = 16, C = DH == 64 ? 128 : 64, NW = 4, KPW = C / NW, STAGES = 4;
-  static constexpr int TILE = C * DH * 2, STAGE = 2 * TILE, RING = STAGES * STAGE;
+  static constexpr int TILE = C * DH * 2, STAGE = 2 * TILE, RING = STAGES * STAGE, Q = 16 * DH * 2;
   static constexpr int STATES = NW * 16 * (DH + 2) * 4;
-  static constexpr int THREADS = 256;                        // four multiplying, four loading warps
-  static constexpr int FIXED = RING + STATES + (int)sizeof(Tree) + 1024 + 256;
-  static int bytes(int batch) { return FIXED + (batch + 1) * 12 + 16; }
+  static constexpr int THREADS = 2 * NW * 32 + 32;
+  static constexpr int FIXED = RING + 2 * Q + STATES + (int)sizeof(Tree) + 1024 + 512;
+  static int bytes(int batch) { return FIXED + plan_bytes(batch); }
 };
 
 template <typename T, int DH>
-__global__ void __launch_bounds__(256, 1) rows16_kernel(const __grid_constant__ Args a) {
+__global__ void __launch_bounds__(Rows16<DH>::THREADS, 1) rows16_kernel(const __grid_constant__ Args a) {
   using CF = Rows16<DH>;
   constexpr int C = CF::C, NW = CF::NW, KPW = CF::KPW, KS = DH / 16, KB = KPW / 16, NT = KPW / 8, ST = CF::STAGES;
   extern __shared__ unsigned char smem_raw[];
   unsigned char* sm = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-  float* pw = reinterpret_cast<float*>(sm + CF::RING);       // [NW][16][DH] outputs
+  unsigned char* sq = sm + CF::RING;                         // [2] queries
+  float* pw = reinterpret_cast<float*>(sq + 2 * CF::Q);      // [NW][16][DH] outputs
   float* ml = pw + NW * 16 * DH;                             // [NW][16][2] maxima and sums
-  Tree& tree = *reinterpret_cast<Tree*>(sm + CF::RING + CF::STATES);
-  uint64_t* full = reinterpret_cast<uint64_t*>(sm + CF::RING + CF::STATES + ((sizeof(Tree) + 7) & ~size_t(7)));
-  uint64_t* empty = full + ST;
-  long long* s_sh = reinterpret_cast<long long*>(empty + ST);              // [16]
-  long long* s_base = s_sh + 16;
-  int* s_tile_base = reinterpret_cast<int*>(s_base + a.batch + 1);
-  __shared__ int s_fail;
+  int4* s_info = reinterpret_cast<int4*>(pw + NW * 16 * (DH + 2));
+  long long* s_base = reinterpret_cast<long long*>(s_info + a.batch);
+  long long* s_sh = s_base + a.batch + 1;                    // [2 * warps]
+  uint64_t* full = reinterpret_cast<uint64_t*>(s_sh + 20);
+  uint64_t *empty = full + ST, *q_full = empty + ST, *q_free = q_full + 2;
+  Tree& tree = *reinterpret_cast<Tree*>(q_free + 2);
+  int* s_tile_base = reinterpret_cast<int*>(&tree + 1);
+  __shared__ int s_fail, s_stop;                             // (s_stop: the multiplying warps' own, read between two of their barriers)
   const int warp = (int)ptx::uniform(threadIdx.x >> 5), lane = threadIdx.x & 31, g = lane >> 2, t4 = lane & 3;
   ptx::grid_dep_launch();
   if (threadIdx.x == 0) {
-    s_fail = 0;
-    for (int i = 0; i < ST; ++i) { ptx::mbar_init(full + i, 128); ptx::mbar_init(empty + i, NW); }
+    s_fail = s_stop = 0;
+    for (int i = 0; i < ST; ++i) { ptx::mbar_init(full + i, 32); ptx::mbar_init(empty + i, NW); }
+    for (int i = 0; i < 2; ++i) { ptx::mbar_init(q_full + i, 32); ptx::mbar_init(q_free + i, 2 * NW); }
     ptx::fence_mbar_init();
   }
   Plan plan;
-  make_plan<C, 16, CF::THREADS>(a, plan, s_base, s_tile_base, s_sh);
+  make_plan<C, 16, CF::THREADS>(a, plan, s_info, s_base, s_tile_base, s_sh);
   Walk<C, 16> w;
   w.init(a, plan, blockIdx.x);
+  auto wait = [](uint64_t* bar, uint32_t parity) { return __all_sync(0xffffffffu, ptx::mbar_wait(bar, parity)) != 0; };
   __syncthreads();
 
-  if (warp >= NW) {
-    // ---- loading: a thread brings piece `piece` of rows r0, r0 + STEP, ...
-    constexpr int PIECES = DH / 8, STEP = 128 / PIECES, RPT = C / STEP;
-    const int t = threadIdx.x - NW * 32, piece = t % PIECES, row0 = t / PIECES;
-    const uint32_t half_off = (uint32_t)(piece >> 3) * C * 128;
-    const T *kc = reinterpret_cast<const T*>(a.k) + piece * 8, *vc = reinterpret_cast<const T*>(a.v) + piece * 8;
-    const T *kn = static_cast<const T*>(a.k_new) + piece * 8, *vn = static_cast<const T*>(a.v_new) + piece * 8;
-    Chunk cur{}, nxt{};
-    int ids[RPT], ids2[RPT];                                 // page ids of the thread's rows (-1: nothing there)
-    int hk = 0, hk2 = 0, r0 = 0, r02 = 0, c = 0;
-    bool more = w.next(a, plan);
-    auto fetch = [&](const Chunk& k, int (&id)[RPT]) {
-      if (k.tree) return;
-      const int* table = a.table + (int64_t)w.s.seq * a.max_pages;
-#pragma unroll
-      for (int i = 0; i < RPT; ++i) {
-        const int r = row0 + i * STEP;
-        id[i] = r < k.n ? __ldg(table + a.page_div(k.start + r)) : -1;
-      }
-    };
-    auto take = [&](Chunk& k, int& h, int& r) {              // the chunk at the walk's place
-      k = chunk_of<C>(w.s, c);
-      h = w.tile / w.s.tiles;
-      r = w.s.r0;
-    };
-    if (more) { c = w.c; take(cur, hk, r0); fetch(cur, ids); }
-    for (int i = 0; more; ++i) {
-      // the next chunk, and its page ids
-      bool more2 = true;
-      if (++c >= w.c_end) { more2 = w.next(a, plan); c = w.c; }
-      if (more2) { take(nxt, hk2, r02); fetch(nxt, ids2); }
-      const int st = i % ST;
-      if (i >= ST && !__all_sync(0xffffffffu, ptx::mbar_wait(empty + st, ((i / ST) - 1) & 1))) { s_fail = 1; break; }
-      const uint32_t Ks = ptx::smem_u32(sm + st * CF::STAGE) + half_off, Vs = Ks + CF::TILE;
-#pragma unroll
-      for (int j = 0; j < RPT; ++j) {
-        const int r = row0 + j * STEP;
-        bool there = r < cur.n;
-        int64_t at = 0;
-        const T *ks = kc, *vs = vc;
-        if (cur.tree) {
-          if (there) at = (int64_t)(r0 + cur.start + r) * a.new_row + hk * DH;
-          ks = kn; vs = vn;
-        } else if (there) {
-          const int s = cur.start + r, id = ids[j];
-          if (id < 0 || id >= a.n_pages) {
-            there = false;
-            if (a.status != nullptr) atomicMin(a.status, FM_ERR_INVALID_ARG);
-          } else {
-            at = id * a.page + hk * a.head + (int64_t)(s - a.page_div(s) * a.page_div.d) * a.slot;
-          }
+  if (warp == 2 * NW) {
+    // ---- loading
+    int i = 0, part = 0, written = 0;                        // chunks left whose place threads have written
+    int4 cut = make_int4(0, 0, 0, 0);
+    long long cut_end = 0;
+    bool ok = true;
+    while (ok && w.next(a, plan)) {
+      const int hk = w.tile / w.s.tiles, mt = w.tile - hk * w.s.tiles;
+      if (w.starts() && !w.ends()) { cut = make_int4(w.b, hk, mt, 1); cut_end = w.tile_start + w.s.chunks + OVER; }
+      if (part >= 2 && !(ok = wait(q_free + (part & 1), ((part >> 1) - 1) & 1))) break;
+      request_queries<T, DH, 16>(a, w.s, hk, mt, sq + (part & 1) * CF::Q, lane);
+      cp_arrive(q_full + (part & 1));
+      ++part;
+      for (int c = w.c; c < w.c_end; ++c, ++i) {
+        const Chunk k = chunk_of<C>(w.s, c);
+        const int st = i % ST;
+        if (i >= ST && !(ok = wait(empty + st, ((i / ST) - 1) & 1))) break;
+        unsigned char* Ks = sm + st * CF::STAGE;
+        if (a.tma && !k.tree) {
+          if (written > 0) { --written; ptx::fence_proxy_async(); }
+          request_boxes<T, DH, C>(a, w.s, k, hk, Ks, Ks + CF::TILE, full + st, lane);
+        } else {
+          request_pieces<T, DH, C>(a, w.s, k, hk, Ks, Ks + CF::TILE, lane);
+          cp_arrive(full + st);
+          written = ST;
         }
-        const uint32_t to = ptx::swz128(r, piece & 7);
-        cp16(Ks + to, ks + at, there);
-        cp16(Vs + to, vs + at, there);
       }
-      cp_arrive(full + st);
-      more = more2;
-      cur = nxt; hk = hk2; r0 = r02;
-#pragma unroll
-      for (int j = 0; j < RPT; ++j) ids[j] = ids2[j];
     }
+    if (!ok) s_fail = 1;
+    write_desc<C, 16>(a, plan, cut, cut_end, lane);
     asm volatile("cp.async.wait_all;" ::: "memory");
   } else {
     // ---- multiplying
-    auto sync = [] { asm volatile("bar.sync 1, 128;" ::: "memory"); };
-    int tree_of = -1, it = 0;
-    if (threadIdx.x == 0) a.desc[blockIdx.x] = make_int4(0, 0, 0, 0);
+    auto sync = [] { asm volatile("bar.sync 1, 256;" ::: "memory"); };
+    const int group = warp >> 2, wg = warp & 3;
+    int tree_of = -1, it = 0, part = 0;
     while (w.next(a, plan)) {
       const Seq& s = w.s;
       const int hk = w.tile / s.tiles, mt = w.tile - hk * s.tiles, M = s.n * a.G;
-      if (tree_of != w.b) { build_tree<128>(tree, a.parent + s.r0, s.n, threadIdx.x, sync); tree_of = w.b; }
-      const bool whole = w.c == 0 && w.c_end == s.chunks;
-      if (threadIdx.x == 0 && w.c == 0 && !whole)
-        a.desc[blockIdx.x] = make_int4(w.b, hk, mt, parts_of<C, 16>(a, plan, blockIdx.x, w.tile_start + s.chunks));
+      if (tree_of != w.b) { build_tree<256>(tree, a.parent + s.r0, s.n, threadIdx.x, sync); tree_of = w.b; }
+      const bool whole = w.starts() && w.ends();
+      bool ok = wait(q_full + (part & 1), (part >> 1) & 1);
       uint32_t qa[KS][4];
-      int node[2];                                           // the rows' nodes, -1: behind the last
+      {
+        const uint32_t q = ptx::smem_u32(sq + (part & 1) * CF::Q);
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+          const int ch = ks * 2 + (lane >> 4);
+          ptx::ldmatrix_x4(qa[ks][0], qa[ks][1], qa[ks][2], qa[ks][3], q + (ch >> 3) * 16 * 128 + ptx::swz128(lane & 15, ch & 7));
+        }
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(q_free + (part & 1));
+        ++part;
+      }
+      // the rows' nodes (-1: behind the last), depths, first cached positions behind the prefix that they see
+      int node[2], depth[2], low[2];
 #pragma unroll
       for (int hr = 0; hr < 2; ++hr) {
         const int idx = mt * 16 + g + hr * 8;
-        const bool ok = idx < M;
-        const int i = ok ? idx / a.G : 0, gh = ok ? idx - i * a.G : 0;
-        node[hr] = ok ? i : -1;
-        const T* qp = static_cast<const T*>(a.q) + (int64_t)(s.r0 + i) * a.q_row + (hk * a.G + gh) * DH;
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-          qa[ks][hr] = ok ? __ldg(reinterpret_cast<const unsigned int*>(qp + ks * 16 + 2 * t4)) : 0u;
-          qa[ks][2 + hr] = ok ? __ldg(reinterpret_cast<const unsigned int*>(qp + ks * 16 + 8 + 2 * t4)) : 0u;
-        }
-      }
-      // first cached position behind the prefix that a row sees
-      int depth[2], low[2];
-#pragma unroll
-      for (int hr = 0; hr < 2; ++hr) {
+        node[hr] = idx < M ? idx / a.G : -1;
         depth[hr] = node[hr] >= 0 ? tree.depth[node[hr]] : 0;
         low[hr] = a.window > 0 ? s.len + depth[hr] - a.window + 1 : 0;
       }
@@ -456,31 +523,35 @@ __global__ void __launch_bounds__(256, 1) rows16_kernel(const __grid_constant__ 
       float mrun[2] = {-INFINITY, -INFINITY}, lrun[2] = {0.f, 0.f};
 #pragma unroll
       for (int i = 0; i < DH / 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
-      bool gave_up = false;
       for (int c = w.c; c < w.c_end; ++c, ++it) {
+        if ((it & 1) != group) continue;
         const Chunk ck = chunk_of<C>(s, c);
         const int st = it % ST;
         const bool uneven = ck.tree || (a.window > 0 && ck.start + ck.n > a.n_prefix && ck.start < low_all);   // rows differ in what they see
         const bool all_vis = !uneven && ck.n == C;
-        if (!__all_sync(0xffffffffu, ptx::mbar_wait(full + st, (it / ST) & 1))) { gave_up = true; break; }
+        if (!(ok = ok && wait(full + st, (it / ST) & 1))) break;
         const uint32_t Ks_u = ptx::smem_u32(sm + st * CF::STAGE), Vs_u = Ks_u + CF::TILE;
         uint32_t kf[KB][KS][4], vf[KB][DH / 16][4];
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
           for (int ks = 0; ks < KS; ++ks) {
-            const int key = warp * KPW + kb * 16 + (lane & 7) + (lane >> 4) * 8;
+            const int key = wg * KPW + kb * 16 + (lane & 7) + (lane >> 4) * 8;
             const int ch = ks * 2 + ((lane >> 3) & 1);
             ptx::ldmatrix_x4(kf[kb][ks][0], kf[kb][ks][1], kf[kb][ks][2], kf[kb][ks][3], Ks_u + (ch >> 3) * C * 128 + ptx::swz128(key, ch & 7));
           }
+        // (128 features: behind the scores, or keys and values together take more registers than there are)
+        auto load_values = [&] {
 #pragma unroll
-        for (int kb = 0; kb < KB; ++kb)
+          for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-          for (int dp = 0; dp < DH / 16; ++dp) {
-            const int key = warp * KPW + kb * 16 + (lane & 7) + ((lane >> 3) & 1) * 8;
-            const int ch = dp * 2 + (lane >> 4);
-            ptx::ldmatrix_x4_trans(vf[kb][dp][0], vf[kb][dp][1], vf[kb][dp][2], vf[kb][dp][3], Vs_u + (ch >> 3) * C * 128 + ptx::swz128(key, ch & 7));
-          }
+            for (int dp = 0; dp < DH / 16; ++dp) {
+              const int key = wg * KPW + kb * 16 + (lane & 7) + ((lane >> 3) & 1) * 8;
+              const int ch = dp * 2 + (lane >> 4);
+              ptx::ldmatrix_x4_trans(vf[kb][dp][0], vf[kb][dp][1], vf[kb][dp][2], vf[kb][dp][3], Vs_u + (ch >> 3) * C * 128 + ptx::swz128(key, ch & 7));
+            }
+        };
+        if (DH == 64) load_values();
         float sc[NT][4];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) sc[nt][0] = sc[nt][1] = sc[nt][2] = sc[nt][3] = 0.f;
@@ -491,10 +562,7 @@ __global__ void __launch_bounds__(256, 1) rows16_kernel(const __grid_constant__ 
             mma16816(sc[2 * kb], qa[ks], kf[kb][ks][0], kf[kb][ks][1], T());
             mma16816(sc[2 * kb + 1], qa[ks], kf[kb][ks][2], kf[kb][ks][3], T());
           }
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) sc[nt][e] *= a.scale_log2;
+        if (DH == 128) load_values();
         bool bad = false;
         if (!all_vis) {
           // keys of this thread: n-tile nt, element e -> nt * 8 + 2 * t4 + e of the warp's slice
@@ -502,7 +570,7 @@ __global__ void __launch_bounds__(256, 1) rows16_kernel(const __grid_constant__ 
           for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-              const int k = warp * KPW + nt * 8 + 2 * t4 + e, at = ck.start + k;
+              const int k = wg * KPW + nt * 8 + 2 * t4 + e, at = ck.start + k;
 #pragma unroll
               for (int hr = 0; hr < 2; ++hr) {
                 bool vis = k < ck.n && node[hr] >= 0;
@@ -511,14 +579,13 @@ __global__ void __launch_bounds__(256, 1) rows16_kernel(const __grid_constant__ 
                 if (!vis) sc[nt][hr * 2 + e] = -INFINITY;
               }
             }
-          if (uneven) {
+          // (what lies behind the length is whatever the page holds)
 #pragma unroll
-            for (int kb = 0; kb < KB; ++kb)
+          for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-              for (int dp = 0; dp < DH / 16; ++dp)
+            for (int dp = 0; dp < DH / 16; ++dp)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) vf[kb][dp][j] = finite_part<T>(vf[kb][dp][j], bad);
-          }
+              for (int j = 0; j < 4; ++j) vf[kb][dp][j] = finite_part<T>(vf[kb][dp][j], bad);
         }
         float scale[2], base[2];
 #pragma unroll
@@ -528,7 +595,7 @@ __global__ void __launch_bounds__(256, 1) rows16_kernel(const __grid_constant__ 
           for (int nt = 0; nt < NT; ++nt) mx = fmaxf(mx, fmaxf(sc[nt][hr * 2], sc[nt][hr * 2 + 1]));
           mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
           mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
-          const float mnew = fmaxf(mrun[hr], mx);
+          const float mnew = fmaxf(mrun[hr], mx * a.scale_log2);
           base[hr] = mnew == -INFINITY ? 0.f : mnew;
           scale[hr] = mnew == mrun[hr] ? 1.f : ex2(mrun[hr] - base[hr]);
           mrun[hr] = mnew;
@@ -538,7 +605,7 @@ __global__ void __launch_bounds__(256, 1) rows16_kernel(const __grid_constant__ 
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            sc[nt][e] = ex2(sc[nt][e] - base[e >> 1]);
+            sc[nt][e] = ex2(fmaf(sc[nt][e], a.scale_log2, -base[e >> 1]));
             ls[e >> 1] += sc[nt][e];
           }
         lrun[0] = lrun[0] * scale[0] + ls[0];
@@ -570,7 +637,7 @@ __global__ void __launch_bounds__(256, 1) rows16_kernel(const __grid_constant__ 
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt)
             for (int k = 0; k < 8; ++k) {
-              const int key = warp * KPW + nt * 8 + k, src = (lane & ~3) | (k >> 1);
+              const int key = wg * KPW + nt * 8 + k, src = (lane & ~3) | (k >> 1);
               const float p0 = __shfl_sync(0xffffffffu, (k & 1) ? sc[nt][1] : sc[nt][0], src);
               const float p1 = __shfl_sync(0xffffffffu, (k & 1) ? sc[nt][3] : sc[nt][2], src);
 #pragma unroll
@@ -587,28 +654,50 @@ __global__ void __launch_bounds__(256, 1) rows16_kernel(const __grid_constant__ 
         __syncwarp();
         if (lane == 0) ptx::mbar_arrive(empty + st);
       }
-      if (gave_up) { s_fail = 1; }
+      if (!ok) s_fail = s_stop = 1;
 #pragma unroll
       for (int hr = 0; hr < 2; ++hr) {
         lrun[hr] += __shfl_xor_sync(0xffffffffu, lrun[hr], 1);
         lrun[hr] += __shfl_xor_sync(0xffffffffu, lrun[hr], 2);
       }
-      // ---- the warps' states, merged in warp order
-      float* mine = pw + warp * 16 * DH;
+      // ---- the states: the odd chunks' to the same warp of the even ones, then those in warp order
+      float* mine = pw + wg * 16 * DH;
+      auto put = [&] {
 #pragma unroll
-      for (int i = 0; i < DH / 8; ++i) {
-        *reinterpret_cast<float2*>(mine + g * DH + i * 8 + 2 * t4) = make_float2(o[i][0], o[i][1]);
-        *reinterpret_cast<float2*>(mine + (g + 8) * DH + i * 8 + 2 * t4) = make_float2(o[i][2], o[i][3]);
-      }
-      if (t4 == 0) {
-        *reinterpret_cast<float2*>(ml + (warp * 16 + g) * 2) = make_float2(mrun[0], lrun[0]);
-        *reinterpret_cast<float2*>(ml + (warp * 16 + g + 8) * 2) = make_float2(mrun[1], lrun[1]);
+        for (int i = 0; i < DH / 8; ++i) {
+          *reinterpret_cast<float2*>(mine + g * DH + i * 8 + 2 * t4) = make_float2(o[i][0], o[i][1]);
+          *reinterpret_cast<float2*>(mine + (g + 8) * DH + i * 8 + 2 * t4) = make_float2(o[i][2], o[i][3]);
+        }
+        if (t4 == 0) {
+          *reinterpret_cast<float2*>(ml + (wg * 16 + g) * 2) = make_float2(mrun[0], lrun[0]);
+          *reinterpret_cast<float2*>(ml + (wg * 16 + g + 8) * 2) = make_float2(mrun[1], lrun[1]);
+        }
+      };
+      if (group == 1) put();
+      sync();
+      if (*reinterpret_cast<volatile int*>(&s_stop)) break;  // (every warp has set its word in front of the barrier: all leave)
+      if (group == 0) {
+#pragma unroll
+        for (int hr = 0; hr < 2; ++hr) {
+          const float2 q = *reinterpret_cast<const float2*>(ml + (wg * 16 + g + 8 * hr) * 2);
+          // (no chunk on one side: maximum -inf and sum 0; a sum that is no number goes through)
+          const float mm = fmaxf(mrun[hr], q.x), f0 = mrun[hr] == -INFINITY ? 1.f : ex2(mrun[hr] - mm), f1 = q.x == -INFINITY ? 1.f : ex2(q.x - mm);
+          lrun[hr] = (f0 == 0.f ? 0.f : lrun[hr] * f0) + (f1 == 0.f ? 0.f : q.y * f1);
+          mrun[hr] = mm;
+#pragma unroll
+          for (int i = 0; i < DH / 8; ++i) {
+            const float2 v = *reinterpret_cast<const float2*>(mine + (g + 8 * hr) * DH + i * 8 + 2 * t4);
+            o[i][2 * hr] = (f0 == 0.f ? 0.f : o[i][2 * hr] * f0) + (f1 == 0.f ? 0.f : v.x * f1);
+            o[i][2 * hr + 1] = (f0 == 0.f ? 0.f : o[i][2 * hr + 1] * f0) + (f1 == 0.f ? 0.f : v.y * f1);
+          }
+        }
+        __syncwarp();
+        put();
       }
       sync();
-      if (*reinterpret_cast<volatile int*>(&s_fail)) break;  // (every warp has set its word in front of the barrier: all leave)
       const int rows_here = min(16, M - mt * 16);
-      float* part = a.part + (size_t)(blockIdx.x * 2 + (w.c == 0 ? 1 : 0)) * 16 * (DH + 2);
-      for (int e = threadIdx.x; e < rows_here * (DH / 2); e += 128) {
+      float* part_at = a.part + (size_t)(blockIdx.x * 2 + (w.starts() ? 1 : 0)) * 16 * (DH + 2);
+      for (int e = threadIdx.x; e < rows_here * (DH / 2); e += 256) {
         const int i = e / (DH / 2), col = 2 * (e - i * (DH / 2)), idx = mt * 16 + i, nd = idx / a.G, gh = idx - nd * a.G;
         const bool live = tree.reach[nd][nd >> 5] != 0u;
         float2 stt[NW];
@@ -617,7 +706,7 @@ __global__ void __launch_bounds__(256, 1) rows16_kernel(const __grid_constant__ 
         for (int k = 0; k < NW; ++k) { stt[k] = *reinterpret_cast<const float2*>(ml + (k * 16 + i) * 2); mm = fmaxf(mm, stt[k].x); }
 #pragma unroll
         for (int k = 0; k < NW; ++k) {
-          const float f = stt[k].x == -INFINITY ? (stt[k].y == stt[k].y ? 0.f : 1.f) : ex2(stt[k].x - mm);
+          const float f = stt[k].x == -INFINITY ? 1.f : ex2(stt[k].x - mm);
           const float2 v = *reinterpret_cast<const float2*>(pw + (k * 16 + i) * DH + col);
           if (f != 0.f) { l += f * stt[k].y; o0 += f * v.x; o1 += f * v.y; }
         }
@@ -627,7 +716,7 @@ __global__ void __launch_bounds__(256, 1) rows16_kernel(const __grid_constant__ 
           *reinterpret_cast<uint32_t*>(static_cast<T*>(a.out) + (int64_t)(s.r0 + nd) * a.out_row + (hk * a.G + gh) * DH + col) = pack(o0 * inv, o1 * inv, T());
           if (col == 0 && a.lse != nullptr) a.lse[(int64_t)(s.r0 + nd) * a.H + hk * a.G + gh] = live ? (mm + log2f(l)) * 0.6931471805599453f : -INFINITY;
         } else {
-          float* row = part + (size_t)i * (DH + 2);
+          float* row = part_at + (size_t)i * (DH + 2);
           *reinterpret_cast<float2*>(row + col) = make_float2(o0, o1);
           if (col == 0) *reinterpret_cast<float2*>(row + DH) = make_float2(mm, l);
         }
@@ -636,12 +725,423 @@ __global__ void __launch_bounds__(256, 1) rows16_kernel(const __grid_constant__ 
     }
   }
   __syncthreads();
-  if (s_fail) {                                              // a bounded wait gave up: report
+  if (s_fail) {                                              // a bounded wait gave up: report, once what was requested has landed
     if (threadIdx.x == 0 && a.status != nullptr) atomicMin(a.status, FM_ERR_TIMEOUT);
+    ptx::drain_delay();
   }
 }
 
-// ---- parts of the tiles that were cut, merged in order: grid (CTAS, ROWS / 4), two warps a row
+// ------------------------------------------------------------------------------------------
+// 128 query rows a tile, on the tensor cores
+// ------------------------------------------------------------------------------------------
+// S = Q K^T and O += P V are tcgen05 MMAs with accumulators in tensor memory; V is multiplied as it lies (keys x features:
+// MN-major), P goes back to tensor memory as the A operand.  Two threads share a row of the softmax and exchange
+// maxima; S of the next chunk is multiplied as soon as S is in registers.  The output is rescaled only when a row's
+// maximum has grown by more than 2^8 (P then stays below 2^8).  Two CTAs per SM: one's softmax
+// runs under the other's MMAs.  One warp requests the chunks' boxes.  A second one (the fixer) brings what boxes do not: queries,
+// nodes, odd pages; it takes values that are not finite out of chunks with hidden keys, and makes its writes visible to
+// the tensor cores by a proxy fence.
+template <int DH>
+struct Rows128 {
+  static constexpr int ROWS = 128, C = 64, STAGES = DH == 64 ? 4 : 2, HC = C / 2;
+  static constexpr int THREADS = 64 + 32 + 256;
+  static constexpr int Q = 128 * DH * 2, TILE = C * DH * 2, STAGE = 2 * TILE;
+  static constexpr int FIXED = Q + STAGES * STAGE + (int)sizeof(Tree) + 512 * 4 + 512 + 1024;
+  static int bytes(int batch) { return FIXED + plan_bytes(batch); }
+};
+constexpr float GROW = 8.f;
+
+__device__ inline uint64_t pack2(float a, float b) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ inline float2 unpack2(uint64_t r) {
+  float2 v;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(v.x), "=f"(v.y) : "l"(r));
+  return v;
+}
+__device__ inline uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ inline uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ inline float max3(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+__device__ inline void st16(uint32_t taddr, const uint32_t (&r)[16]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};" ::"r"(r[0]), "r"(r[1]),
+               "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]),
+               "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(taddr)
+               : "memory");
+}
+__device__ inline void ld32(uint32_t taddr, uint32_t* r) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,"
+      "%28,%29,%30,%31}, [%32];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
+        "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]),
+        "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]),
+        "=r"(r[31])
+      : "r"(taddr));
+}
+__device__ inline void ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ inline void st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ inline void mma_ts(uint32_t d, uint32_t a, uint64_t db, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
+      "r"(a), "l"(db), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+// fp32 accumulate, A and B of type T, M = 128, N = n
+template <typename T>
+__device__ constexpr uint32_t instr_desc(int n) {
+  return (1u << 4) | (__is_same(T, bf16) ? (1u << 7) | (1u << 10) : 0u) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
+}
+
+// Can a chunk hold keys that some row does not see?  (The deepest node has fewer ancestors than the tree has nodes.  What lies
+// behind the length is whatever the page holds.)
+template <int C>
+__device__ inline bool uneven_chunk(const Args& a, const Seq& s, const Chunk& k) {
+  return k.tree || k.n < C || (a.window > 0 && k.start + k.n > a.n_prefix && k.start < s.len + s.n - a.window);
+}
+// values of a key: where they are, null if its page is none
+template <typename T, int DH>
+__device__ inline const T* values_of(const Args& a, const Seq& s, const Chunk& k, int hk, int key) {
+  if (k.tree) return static_cast<const T*>(a.v_new) + (int64_t)(s.r0 + k.start + key) * a.new_row + hk * DH;
+  const int at = k.start + key, pi = a.page_div(at), id = a.table[(int64_t)s.seq * a.max_pages + pi];
+  if (id < 0 || id >= a.n_pages) return nullptr;
+  return reinterpret_cast<const T*>(a.v) + id * a.page + hk * a.head + (int64_t)(at - pi * a.page_div.d) * a.slot;
+}
+
+template <typename T, int DH>
+__global__ void __launch_bounds__(Rows128<DH>::THREADS, 2) rows128_kernel(const __grid_constant__ Args a) {
+  using CF = Rows128<DH>;
+  constexpr int C = CF::C, HC = CF::HC, ST = CF::STAGES, TILE = CF::TILE, STAGE = CF::STAGE;
+  extern __shared__ unsigned char smem_raw[];
+  unsigned char* sm = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+  unsigned char* ring = sm + CF::Q;                          // behind the queries
+  float* s_pair = reinterpret_cast<float*>(ring + ST * STAGE);             // [use mod 2][half][row]
+  int4* s_info = reinterpret_cast<int4*>(s_pair + 512);
+  long long* s_base = reinterpret_cast<long long*>(s_info + a.batch);
+  long long* s_sh = s_base + a.batch + 1;                    // [2 * warps]
+  uint64_t* full = reinterpret_cast<uint64_t*>(s_sh + 24);
+  uint64_t *fixed = full + ST, *empty = fixed + ST, *q_full = empty + ST, *q_free = q_full + 1, *s_full = q_free + 1, *s_read = s_full + 1, *p_full = s_read + 1,
+           *o_full = p_full + 1, *done = o_full + 1;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(done + 1);
+  Tree& tree = *reinterpret_cast<Tree*>(done + 2);
+  int* s_tile_base = reinterpret_cast<int*>(&tree + 1);
+  __shared__ int s_fail, s_bad;
+  const int warp = (int)ptx::uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
+  ptx::grid_dep_launch();
+  if (threadIdx.x == 0) {
+    s_fail = s_bad = 0;
+    for (int i = 0; i < ST; ++i) { ptx::mbar_init(full + i, 32); ptx::mbar_init(fixed + i, 32); ptx::mbar_init(empty + i, 1); }
+    ptx::mbar_init(q_full, 32); ptx::mbar_init(q_free, 1); ptx::mbar_init(s_full, 1); ptx::mbar_init(s_read, 8); ptx::mbar_init(p_full, 8);
+    ptx::mbar_init(o_full, 1); ptx::mbar_init(done, 1);
+    ptx::fence_mbar_init();
+  }
+  if (warp == 2) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(ptx::smem_u32(tmem_slot)), "r"(256) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  Plan plan;
+  make_plan<C, 128, CF::THREADS>(a, plan, s_info, s_base, s_tile_base, s_sh);
+  Walk<C, 128> w;
+  w.init(a, plan, blockIdx.x);
+  tc::fence_before();
+  __syncthreads();
+  tc::fence_after();
+  const uint32_t tmem = ptx::uniform(*tmem_slot), tO = tmem + C, tP = tO + DH;             // S in columns 0 .. C-1, then O, then P
+  auto wait = [](uint64_t* bar, uint32_t parity) { return __all_sync(0xffffffffu, ptx::mbar_wait(bar, parity)) != 0; };
+
+  if (warp == 0) {
+    // ---- requesting
+    int i = 0;
+    int4 cut = make_int4(0, 0, 0, 0);
+    long long cut_end = 0;
+    bool ok = true;
+    while (ok && w.next(a, plan)) {
+      const int hk = w.tile / w.s.tiles;
+      if (w.starts() && !w.ends()) { cut = make_int4(w.b, hk, w.tile - hk * w.s.tiles, 1); cut_end = w.tile_start + w.s.chunks + OVER; }
+      for (int c = w.c; c < w.c_end; ++c, ++i) {
+        const Chunk k = chunk_of<C>(w.s, c);
+        const int st = i % ST;
+        if (i >= ST && !(ok = wait(empty + st, ((i / ST) - 1) & 1))) break;
+        if (a.tma && !k.tree) request_boxes<T, DH, C>(a, w.s, k, hk, ring + st * STAGE, ring + st * STAGE + TILE, full + st, lane);
+        else ptx::mbar_arrive(full + st);                    // the fixer brings it
+      }
+    }
+    if (!ok) s_fail = 1;
+    write_desc<C, 128>(a, plan, cut, cut_end, lane);
+  } else if (warp == 1) {
+    // ---- fixing
+    int i = 0, part = 0;
+    bool ok = true;
+    while (ok && w.next(a, plan)) {
+      const int hk = w.tile / w.s.tiles;
+      // the tile's queries, once the scores of the tile before have been multiplied
+      if (part > 0 && !(ok = wait(q_free, (part - 1) & 1))) break;
+      request_queries<T, DH, 128>(a, w.s, hk, w.tile - hk * w.s.tiles, sm, lane);
+      asm volatile("cp.async.wait_all;" ::: "memory");
+      ptx::fence_proxy_async();
+      ptx::mbar_arrive(q_full);
+      ++part;
+      for (int c = w.c; c < w.c_end; ++c, ++i) {
+        const Chunk k = chunk_of<C>(w.s, c);
+        const int st = i % ST;
+        unsigned char* Vs = ring + st * STAGE + TILE;
+        if (i >= ST && !(ok = wait(empty + st, ((i / ST) - 1) & 1))) break;
+        const bool uneven = uneven_chunk<C>(a, w.s, k);
+        if (k.tree || !a.tma) {
+          request_pieces<T, DH, C>(a, w.s, k, hk, ring + st * STAGE, Vs, lane);
+          asm volatile("cp.async.wait_all;" ::: "memory");
+          __syncwarp();
+        } else if (uneven) {
+          if (!(ok = wait(full + st, (i / ST) & 1))) break;
+        }
+        if (uneven) {
+          bool bad = false;
+          for (int j = lane; j < TILE / 16; j += 32) {
+            uint4 v = reinterpret_cast<uint4*>(Vs)[j];
+            bool here = false;
+            v.x = finite_part<T>(v.x, here); v.y = finite_part<T>(v.y, here); v.z = finite_part<T>(v.z, here); v.w = finite_part<T>(v.w, here);
+            if (here) { reinterpret_cast<uint4*>(Vs)[j] = v; bad = true; }
+          }
+          if (bad) *reinterpret_cast<volatile int*>(&s_bad) = 1;
+        }
+        if (uneven || !a.tma) ptx::fence_proxy_async();
+        ptx::mbar_arrive(fixed + st);
+      }
+    }
+    if (!ok) s_fail = 1;
+    asm volatile("cp.async.wait_all;" ::: "memory");
+  } else if (warp == 2) {
+    // ---- multiplying
+    const uint32_t id_s = instr_desc<T>(C), id_o = instr_desc<T>(64) | (1u << 16);          // B of P V is MN-major
+    const uint64_t dq = tc::smem_desc_sw128(ptx::smem_u32(sm));
+    int it = 0;
+    bool ok = true;
+    int part = 0;
+    auto scores = [&](int i, bool first, bool last) {
+      const int st = i % ST;
+      if (first && !wait(q_full, part++ & 1)) return false;
+      if (!wait(full + st, (i / ST) & 1) || !wait(fixed + st, (i / ST) & 1)) return false;
+      tc::fence_after();
+      const uint64_t dk = tc::smem_desc_sw128(ptx::smem_u32(ring + st * STAGE));
+      if (ptx::elect_one()) {
+#pragma unroll
+        for (int k = 0; k < DH / 16; ++k)                    // 64 features a half, 16 a step
+          tc::mma_ss(tmem, dq + (k >> 2) * (128 * 128 / 16) + 2 * (k & 3), dk + (k >> 2) * (C * 128 / 16) + 2 * (k & 3), id_s, k > 0 ? 1u : 0u);
+        tc::commit(s_full);
+        if (last) tc::commit(q_free);
+      }
+      return true;
+    };
+    bool more = w.next(a, plan);
+    int c = w.c;
+    if (more) ok = scores(0, true, c + 1 == w.c_end);
+    while (more && ok) {
+      const bool first = c == w.c, last = c + 1 == w.c_end;
+      const int st = it % ST;
+      if (!(ok = wait(s_read, it & 1))) break;
+      if (last) { more = w.next(a, plan); c = w.c; } else { ++c; }
+      if (more && !(ok = scores(it + 1, last, c + 1 == w.c_end))) break;
+      if (!(ok = wait(p_full, it & 1))) break;
+      tc::fence_after();
+      const uint64_t dv = tc::smem_desc_sw128(ptx::smem_u32(ring + st * STAGE + TILE));
+      if (ptx::elect_one()) {
+#pragma unroll
+        for (int h = 0; h < DH / 64; ++h)
+#pragma unroll
+          for (int k = 0; k < C / 16; ++k) mma_ts(tO + 64 * h, tP + 8 * k, dv + h * (C * 128 / 16) + 128 * k, id_o, (!first || k > 0) ? 1u : 0u);
+        tc::commit(empty + st);
+        tc::commit(o_full);
+      }
+      ++it;
+    }
+    if (!ok) s_fail = 1;
+    if (ptx::elect_one()) tc::commit(done);                  // what was issued ends before the CTA does
+    wait(done, 0);
+  } else {
+    // ---- softmax: warps w and w + 4 share 32 query rows, half of a chunk's keys each
+    const int w4 = warp & 3, half = (warp - 3) >> 2, i_row = w4 * 32 + lane, tid = threadIdx.x - 96;
+    const uint32_t lanes = (uint32_t)(w4 * 32) << 16;
+    auto sync = [] { asm volatile("bar.sync 5, 256;" ::: "memory"); };
+    auto meet = [&] { asm volatile("bar.sync %0, 64;" ::"r"(1 + w4) : "memory"); };
+    const float sc = a.scale_log2;
+    int tree_of = -1, it = 0, x = 0;
+    bool ok = true;
+    while (w.next(a, plan)) {
+      const Seq& s = w.s;
+      const int hk = w.tile / s.tiles, mt = w.tile - hk * s.tiles, idx = mt * 128 + i_row, M = s.n * a.G;
+      if (tree_of != w.b) { build_tree<256>(tree, a.parent + s.r0, s.n, tid, sync); tree_of = w.b; }
+      const bool whole = w.starts() && w.ends();
+      const bool there = idx < M;
+      const int node = there ? idx / a.G : 0, gh = there ? idx - node * a.G : 0, depth = there ? tree.depth[node] : 0;
+      const int low = a.window > 0 ? s.len + depth - a.window + 1 : 0, low_all = a.window > 0 ? s.len + tree.max_depth - a.window + 1 : 0;
+      auto visible = [&](const Chunk& ck, int k0) {          // keys k0 .. k0 + 31 of a chunk, a bit each (k0 and a tree's chunks start at multiples of 32)
+        auto below = [](int n) { return n <= 0 ? 0u : (n >= 32 ? ~0u : (1u << n) - 1u); };
+        const int at = ck.start + k0;
+        if (!there) return 0u;
+        if (!ck.tree) return (below(a.n_prefix - at) | ~below(low - at)) & below(ck.n - k0);
+        if (k0 >= ck.n) return 0u;
+        uint32_t bits = tree.reach[node][at >> 5];
+        if (a.window > 0 && depth >= a.window)
+          for (uint32_t left = bits; left != 0u; left &= left - 1u)
+            if (depth - tree.depth[at + __ffs(left) - 1] >= a.window) bits &= ~(left & (0u - left));
+        return bits;
+      };
+      float m = -INFINITY, l = 0.f;                          // the maximum in use (times scale, base 2), this half's sum
+      for (int c = w.c; c < w.c_end; ++c, ++it) {
+        const Chunk ck = chunk_of<C>(s, c);
+        const bool first = c == w.c;
+        const bool all_vis = !ck.tree && ck.n == C && !(a.window > 0 && ck.start + C > a.n_prefix && ck.start < low_all);
+        ok = ok && wait(s_full, it & 1);                     // (goes on: its partner waits at the barrier)
+        tc::fence_after();
+        uint32_t r[HC];
+#pragma unroll
+        for (int j = 0; j < HC; j += 32) ld32(tmem + lanes + HC * half + j, r + j);
+        ld_wait();
+        tc::fence_before();
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(s_read);
+        if (!all_vis) {
+          const uint32_t bits = visible(ck, HC * half);
+#pragma unroll
+          for (int j = 0; j < HC; ++j)
+            if (!((bits >> j) & 1u)) r[j] = 0xff800000u;     // -inf: exponential 0
+        }
+        float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+        for (int j = 0; j < HC; j += 8)
+#pragma unroll
+          for (int k = 0; k < 4; ++k) m4[k] = max3(m4[k], __uint_as_float(r[j + 2 * k]), __uint_as_float(r[j + 2 * k + 1]));
+        float mx = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * sc;
+        float* pair = s_pair + (x++ & 1) * 256;              // (two of them: written again behind the next use's barrier)
+        pair[half * 128 + i_row] = mx;
+        meet();
+        mx = fmaxf(mx, pair[(half ^ 1) * 128 + i_row]);
+        // P of the chunk before has been multiplied: its place, and O, are free
+        if (!first) ok = ok && wait(o_full, (it - 1) & 1);
+        tc::fence_after();
+        const bool grow = mx > m + GROW || (m == -INFINITY && mx != -INFINITY);
+        if (__any_sync(0xffffffffu, grow)) {
+          const float mn = grow ? mx : m, f = m == -INFINITY ? (grow ? 0.f : 1.f) : ex2(m - mn);
+          m = mn;
+          l *= f;
+          if (!first) {                                      // this half's columns of the output
+#pragma unroll 1
+            for (int j = 0; j < DH / 2; j += 16) {
+              uint32_t o[16];
+              tc::ld16(tO + lanes + DH / 2 * half + j, o);
+#pragma unroll
+              for (int k = 0; k < 16; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * f);
+              st16(tO + lanes + DH / 2 * half + j, o);
+            }
+          }
+        }
+        const float base = m == -INFINITY ? 0.f : m;
+        const uint64_t nb = pack2(-base, -base), s2 = pack2(sc, sc);
+        uint64_t sum[2] = {0ull, 0ull};
+#pragma unroll
+        for (int j = 0; j < HC; j += 32) {
+          uint32_t pk[16];
+#pragma unroll
+          for (int k = 0; k < 16; ++k) {
+            const float2 d = unpack2(fma2(pack2(__uint_as_float(r[j + 2 * k]), __uint_as_float(r[j + 2 * k + 1])), s2, nb));
+            const float e0 = ex2(d.x), e1 = ex2(d.y);
+            sum[k & 1] = add2(sum[k & 1], pack2(e0, e1));
+            pk[k] = pack(e0, e1, T());
+          }
+          st16(tP + lanes + (HC * half + j) / 2, pk);
+        }
+        const float2 sa = unpack2(sum[0]), sb = unpack2(sum[1]);
+        l += (sa.x + sa.y) + (sb.x + sb.y);
+        st_wait();
+        tc::fence_before();
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(p_full);
+      }
+      float* pair = s_pair + (x++ & 1) * 256;
+      pair[half * 128 + i_row] = l;
+      meet();
+      l += pair[(half ^ 1) * 128 + i_row];
+      ok = ok && wait(o_full, (it - 1) & 1);
+      tc::fence_after();
+      const bool live = there && tree.reach[node][node >> 5] != 0u;
+      const float inv = live ? 1.f / l : 0.f;
+      T* op = static_cast<T*>(a.out) + (int64_t)(s.r0 + node) * a.out_row + (hk * a.G + gh) * DH;
+      float* part = a.part + ((size_t)(blockIdx.x * 2 + (w.starts() ? 1 : 0)) * 128 + i_row) * (DH + 2);
+#pragma unroll 1
+      for (int j0 = DH / 2 * half; j0 < DH / 2 * (half + 1); j0 += 32) {
+        uint32_t o[32];
+        __syncwarp();
+        ld32(tO + lanes + j0, o);
+        ld_wait();
+        if (*reinterpret_cast<volatile int*>(&s_bad) != 0 && there) {
+          // values that are not finite, for the rows that see their key (p > 0)
+          for (int c = w.c; c < w.c_end; ++c) {
+            const Chunk ck = chunk_of<C>(s, c);
+            if (!uneven_chunk<C>(a, s, ck)) continue;
+            for (int k = 0; k < ck.n; ++k) {
+              if (!((visible(ck, k & ~31) >> (k & 31)) & 1u)) continue;
+              const T* v = values_of<T, DH>(a, s, ck, hk, k);
+              if (v == nullptr) continue;
+#pragma unroll
+              for (int q = 0; q < 16; ++q) {
+                const float2 u = unpack(reinterpret_cast<const uint32_t*>(v + j0)[q], T());
+                if (!(fabsf(u.x) < INFINITY)) o[2 * q] = __float_as_uint(__uint_as_float(o[2 * q]) + u.x);
+                if (!(fabsf(u.y) < INFINITY)) o[2 * q + 1] = __float_as_uint(__uint_as_float(o[2 * q + 1]) + u.y);
+              }
+            }
+          }
+        }
+        if (!ok || !there) {
+        } else if (whole) {
+#pragma unroll
+          for (int j = 0; j < 32; j += 8) {
+            uint32_t p[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k)                      // (a row out of use: zeros, whatever the product holds)
+              p[k] = live ? pack(__uint_as_float(o[j + 2 * k]) * inv, __uint_as_float(o[j + 2 * k + 1]) * inv, T()) : 0u;
+            *reinterpret_cast<uint4*>(op + j0 + j) = make_uint4(p[0], p[1], p[2], p[3]);
+          }
+        } else {
+#pragma unroll
+          for (int j = 0; j < 32; j += 2)
+            *reinterpret_cast<float2*>(part + j0 + j) = live ? make_float2(__uint_as_float(o[j]), __uint_as_float(o[j + 1])) : make_float2(0.f, 0.f);
+        }
+      }
+      if (ok && there && half == 0) {
+        if (!whole) *reinterpret_cast<float2*>(part + DH) = live ? make_float2(m, l) : make_float2(-INFINITY, 0.f);
+        else if (a.lse != nullptr) a.lse[(int64_t)(s.r0 + node) * a.H + hk * a.G + gh] = live ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
+      }
+      tc::fence_before();                                    // (O is read: the next tile's first product, behind this warp's p_full, may replace it)
+    }
+    if (!ok) s_fail = 1;
+  }
+  __syncwarp();
+  tc::fence_before();
+  __syncthreads();
+  tc::fence_after();
+  if (s_fail) {                                              // a bounded wait gave up: report, once what was requested has landed
+    if (threadIdx.x == 0 && a.status != nullptr) atomicMin(a.status, FM_ERR_TIMEOUT);
+    ptx::drain_delay();
+  }
+  if (warp == 2) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(256) : "memory");
+}
+
+// ---- parts of the tiles that were cut, merged in order: grid (CTAs, blocks per tile), two warps a row, four rows at a time
 template <typename T, int DH, int ROWS>
 __global__ void __launch_bounds__(256) merge_kernel(const __grid_constant__ Args a) {
   constexpr int CL = DH / 32, GS = ROWS * (DH + 2);
@@ -650,61 +1150,61 @@ __global__ void __launch_bounds__(256) merge_kernel(const __grid_constant__ Args
   ptx::grid_dep_wait();
   const int4 d = __ldcg(a.desc + blockIdx.x);
   if (d.w < 2) return;
-  const int r0 = a.row_off[d.x], n = min(a.row_off[d.x + 1] - r0, a.max_nodes), M = n * a.G;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, r = warp & 3, half = warp >> 2, i = blockIdx.y * 4 + r, idx = d.z * ROWS + i;
-  if (d.z * ROWS + (int)blockIdx.y * 4 >= M) return;
-  const bool there = idx < M;
-  float m = -INFINITY, l = 0.f, o[CL];
+  const int r0 = a.row_off[d.x], n = min(a.row_off[d.x + 1] - r0, a.max_nodes), rows = min(ROWS, n * a.G - d.z * ROWS);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, r = warp & 3, half = warp >> 2;
+  for (int i0 = blockIdx.y * 4; i0 < rows; i0 += gridDim.y * 4) {
+    const int i = i0 + r, idx = d.z * ROWS + i;
+    const bool there = i < rows;
+    float m = -INFINITY, l = 0.f, o[CL];
 #pragma unroll
-  for (int j = 0; j < CL; ++j) o[j] = 0.f;
-  auto add = [&](float m2, float l2, const float (&o2)[CL]) {
-    if (m2 == -INFINITY && l2 == 0.f) return;
-    const float mn = fmaxf(m, m2), f1 = m == -INFINITY && l == 0.f ? 0.f : ex2(m - mn), f2 = m2 == -INFINITY ? 1.f : ex2(m2 - mn);
-    l = (f1 == 0.f ? 0.f : l * f1) + l2 * f2;
+    for (int j = 0; j < CL; ++j) o[j] = 0.f;
+    auto add = [&](float m2, float l2, const float (&o2)[CL]) {
+      if (m2 == -INFINITY && l2 == 0.f) return;
+      const float mn = fmaxf(m, m2), f1 = m == -INFINITY && l == 0.f ? 0.f : ex2(m - mn), f2 = m2 == -INFINITY ? 1.f : ex2(m2 - mn);
+      l = (f1 == 0.f ? 0.f : l * f1) + l2 * f2;
 #pragma unroll
-    for (int j = 0; j < CL; ++j) o[j] = (f1 == 0.f ? 0.f : o[j] * f1) + (f2 == 0.f ? 0.f : o2[j] * f2);
-    m = mn;
-  };
-  if (there) {
-    constexpr int U = 4;
-    for (int k0 = half; k0 < d.w; k0 += 2 * U) {
-      float2 ml[U];
-      float v[U][CL];
+      for (int j = 0; j < CL; ++j) o[j] = (f1 == 0.f ? 0.f : o[j] * f1) + (f2 == 0.f ? 0.f : o2[j] * f2);
+      m = mn;
+    };
+    if (there) {
+      constexpr int U = 4;
+      for (int k0 = half; k0 < d.w; k0 += 2 * U) {
+        float2 ml[U];
+        float v[U][CL];
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int k = k0 + 2 * u;
-        if (k >= d.w) continue;
-        const float* row = a.part + ((size_t)(blockIdx.x + k) * 2 + (k == 0 ? 1 : 0)) * GS + (size_t)i * (DH + 2);
-        ml[u] = __ldcg(reinterpret_cast<const float2*>(row + DH));
+        for (int u = 0; u < U; ++u) {
+          const int k = k0 + 2 * u;
+          if (k >= d.w) continue;
+          const float* row = a.part + ((size_t)(blockIdx.x + k) * 2 + (k == 0 ? 1 : 0)) * GS + (size_t)i * (DH + 2);
+          ml[u] = __ldcg(reinterpret_cast<const float2*>(row + DH));
 #pragma unroll
-        for (int j = 0; j < CL; ++j) v[u][j] = __ldcg(row + lane + 32 * j);
+          for (int j = 0; j < CL; ++j) v[u][j] = __ldcg(row + lane + 32 * j);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+          if (k0 + 2 * u < d.w) add(ml[u].x, ml[u].y, v[u]);
       }
-#pragma unroll
-      for (int u = 0; u < U; ++u)
-        if (k0 + 2 * u < d.w) add(ml[u].x, ml[u].y, v[u]);
     }
-  }
-  if (half == 1) {
+    __syncthreads();                                         // (the rows before have been read)
+    if (half == 1) {
 #pragma unroll
-    for (int j = 0; j < CL; ++j) s_o[r][lane + 32 * j] = o[j];
-    if (lane == 0) s_ml[r] = make_float2(m, l);
-  }
-  __syncthreads();
-  if (half == 1 || !there) return;
-  float o2[CL];
+      for (int j = 0; j < CL; ++j) s_o[r][lane + 32 * j] = o[j];
+      if (lane == 0) s_ml[r] = make_float2(m, l);
+    }
+    __syncthreads();
+    if (half == 1 || !there) continue;
+    float o2[CL];
 #pragma unroll
-  for (int j = 0; j < CL; ++j) o2[j] = s_o[r][lane + 32 * j];
-  add(s_ml[r].x, s_ml[r].y, o2);
-  const int nd = idx / a.G, gh = idx - nd * a.G, h = d.y * a.G + gh;
-  const bool live = !(m == -INFINITY && l == 0.f);           // (a node in use sees itself)
-  const float inv = live ? 1.f / l : 0.f;
-  T* out = static_cast<T*>(a.out) + (int64_t)(r0 + nd) * a.out_row + (int64_t)h * DH;
+    for (int j = 0; j < CL; ++j) o2[j] = s_o[r][lane + 32 * j];
+    add(s_ml[r].x, s_ml[r].y, o2);
+    const int nd = idx / a.G, gh = idx - nd * a.G, h = d.y * a.G + gh;
+    const bool live = !(m == -INFINITY && l == 0.f);         // (a node in use sees itself)
+    const float inv = live ? 1.f / l : 0.f;
+    T* out = static_cast<T*>(a.out) + (int64_t)(r0 + nd) * a.out_row + (int64_t)h * DH;
 #pragma unroll
-  for (int j = 0; j < CL; ++j) {
-    const uint32_t v = pack(o[j] * inv, 0.f, T());
-    reinterpret_cast<unsigned short*>(out)[lane + 32 * j] = (unsigned short)v;
+    for (int j = 0; j < CL; ++j) reinterpret_cast<unsigned short*>(out)[lane + 32 * j] = (unsigned short)pack(o[j] * inv, 0.f, T());
+    if (lane == 0 && a.lse != nullptr) a.lse[(int64_t)(r0 + nd) * a.H + h] = live ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
   }
-  if (lane == 0 && a.lse != nullptr) a.lse[(int64_t)(r0 + nd) * a.H + h] = live ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
 }
 
 // ------------------------------------------------------------------------------------------

@@ -8,6 +8,9 @@ from __future__ import annotations
 
 import ctypes as C
 import math
+import struct
+
+import torch
 
 from . import binding as _b
 from .binding import FmError
@@ -16,6 +19,7 @@ FM_BF16, FM_FP16, FM_FP32 = 0, 1, 2
 FM_MAX_TOP = 32
 FM_MAX_TREE_NODES = 256
 FM_MAX_SEQS = 4096
+FM_MAX_TREES = 1024
 
 
 class FmCache(C.Structure):
@@ -27,6 +31,10 @@ class FmCache(C.Structure):
 class FmPages(C.Structure):
     _fields_ = [("n_pages", C.c_int32), ("page_slots", C.c_int32), ("max_seqs", C.c_int32), ("max_pages", C.c_int32), ("table", C.c_void_p),
                 ("lens", C.c_void_p), ("refs", C.c_void_p), ("status", C.c_void_p), ("work", C.c_void_p)]
+
+
+# FmNewRows and FmTreeArgs as struct.pack writes them (native sizes and alignment)
+_ROWS, _TREE = struct.Struct("PPqqq"), struct.Struct("PPPPPqqqPPPPPPiiiiiiiif0P")
 
 
 class FmNewRows(C.Structure):
@@ -56,11 +64,11 @@ def _lib():
                 ("fm_pages_reset", C.c_int, [pages, vp]),
                 ("fm_pages_fork", C.c_int, [pages, vp, vp, i32, vp]),
                 ("fm_pages_reserve", C.c_int, [pages, cache, vp, vp, i32, vp]),
-                ("fm_pages_append", C.c_int, [pages, cache, C.POINTER(FmNewRows), vp, vp, vp, i32, vp, i32, i32, vp]),
+                ("fm_pages_append", C.c_int, [pages, cache, C.c_char_p, vp, vp, vp, i32, vp, i32, i32, vp]),
                 ("fm_pages_truncate", C.c_int, [pages, vp, vp, i32, vp]),
                 ("fm_pages_compact", C.c_int, [pages, cache, vp, vp]),
-                ("fm_tree_attention_bytes", C.c_size_t, [cache, C.POINTER(FmTreeArgs)]),
-                ("fm_tree_attention", C.c_int, [cache, i32, C.POINTER(FmTreeArgs), vp, C.c_size_t, vp]),
+                ("fm_tree_attention_bytes", C.c_size_t, [cache, C.c_char_p]),
+                ("fm_tree_attention", C.c_int, [cache, i32, C.c_char_p, vp, C.c_size_t, vp]),
                 ("fm_tree_accept", C.c_int, [vp, vp, vp, vp, i32, vp, i32, vp, vp, vp]),
                 ("fm_logprobs", C.c_int, [vp, i32, i32, i32, i64, vp, vp, vp, vp, i32, vp, vp, vp])):
             getattr(lib, name).restype, getattr(lib, name).argtypes = res, args
@@ -80,18 +88,22 @@ def _check(rc, where):
 
 def _ids(t, device, what):
     """Address of a contiguous int32 vector or matrix on the device."""
-    _need(t.device == device and str(t.dtype) == "torch.int32" and t.is_contiguous(), f"{what}: a contiguous int32 tensor on {device}")
+    if t.dtype is not torch.int32 or t.device != device or not t.is_contiguous():
+        raise FmError(-1, f"{what}: a contiguous int32 tensor on {device}")
     return t.data_ptr()
 
 
-def _on(device, call, *args):
-    """call(*args, stream) on torch's current stream of the device, with the device current."""
-    import torch
-    stream = torch.cuda.current_stream(device).cuda_stream
-    if torch.cuda.current_device() == device.index:
-        return call(*args, stream)
-    with torch.cuda.device(device):
-        return call(*args, stream)
+# A decode loop makes a handful of these calls per pass, each of which takes the device a few microseconds: the address of
+# the current stream without the Stream object around it (2 us), argument blocks packed instead of filled field by field.
+_stream_of = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+
+
+def _on(index, call, *args):
+    """call(*args, stream) on torch's current stream of device `index`, with the device current."""
+    if torch.cuda.current_device() == index:
+        return call(*args, _stream_of(index))
+    with torch.cuda.device(index):
+        return call(*args, _stream_of(index))
 
 
 class PagedCache:
@@ -102,7 +114,6 @@ class PagedCache:
     Calls on one cache have to be ordered: one stream, or streams that wait for one another."""
 
     def __init__(self, n_layers, n_pages, page_slots, n_kv_heads, head_dim, max_seqs, max_pages, dtype=None, device="cuda:0"):
-        import torch
         if not torch.cuda.is_available():
             raise RuntimeError("PagedCache needs a CUDA device; there is no CPU path")
         shape = (n_layers, n_pages, n_kv_heads, page_slots, head_dim)
@@ -118,7 +129,6 @@ class PagedCache:
         return self
 
     def _lay(self, k, v, table, lens, refs):
-        import torch
         types = {torch.bfloat16: FM_BF16, torch.float16: FM_FP16}
         _need(k.dim() == 5 and k.is_cuda and k.dtype in types and k.shape == v.shape and k.dtype == v.dtype and k.device == v.device,
               "PagedCache: k and v [layers, pages, kv heads, slots, head_dim] in bfloat16 or float16 on one device")
@@ -138,6 +148,7 @@ class PagedCache:
                               self.head_dim, types[k.dtype])
         self._pages = FmPages(self.n_pages, self.page_slots, self.max_seqs, self.max_pages, _ids(table, self.device, "table"),
                               _ids(lens, self.device, "lens"), _ids(refs, self.device, "refs"), self.status.data_ptr(), self.work.data_ptr())
+        self._sizes = {}                                   # workspace bytes by (heads, max_nodes)
         self._cache_p, self._pages_p = C.byref(self._cache), C.byref(self._pages)
 
     def _list(self, a, b, what):
@@ -153,17 +164,17 @@ class PagedCache:
 
     def reset(self):
         """All pages free, all sequences empty."""
-        _check(_on(self.device, _lib().fm_pages_reset, self._pages_p), "fm_pages_reset")
+        _check(_on(self.device.index, _lib().fm_pages_reset, self._pages_p), "fm_pages_reset")
 
     def fork(self, src, dst):
         """Sequences dst become copies of src that share their pages (int32 lists on the device; negative: skipped)."""
         s, d, n = self._list(src, dst, "fork")
-        _check(_on(self.device, _lib().fm_pages_fork, self._pages_p, s, d, n), "fm_pages_fork")
+        _check(_on(self.device.index, _lib().fm_pages_fork, self._pages_p, s, d, n), "fm_pages_fork")
 
     def reserve(self, seqs, grow):
         """Pages of their own for grow[i] more positions of sequence seqs[i] (a shared last page is copied)."""
         s, g, n = self._list(seqs, grow, "reserve")
-        _check(_on(self.device, _lib().fm_pages_reserve, self._pages_p, self._cache_p, s, g, n), "fm_pages_reserve")
+        _check(_on(self.device.index, _lib().fm_pages_reserve, self._pages_p, self._cache_p, s, g, n), "fm_pages_reserve")
 
     def append(self, seqs, k_new, v_new, row_off, path=None, n_acc=None, max_rows=None):
         """Write rows of k_new, v_new [layers, rows, kv heads, head_dim] behind the sequences and advance their lengths: all rows
@@ -181,21 +192,20 @@ class PagedCache:
         if max_rows is None:
             max_rows = stride if path is not None else k_new.shape[1]
         s = k_new.stride()
-        rows = FmNewRows(k_new.data_ptr(), v_new.data_ptr(), s[0], s[1], s[2])
-        _check(_on(self.device, _lib().fm_pages_append, self._pages_p, self._cache_p, C.byref(rows), _ids(seqs, self.device, "seqs"),
+        rows = _ROWS.pack(k_new.data_ptr(), v_new.data_ptr(), s[0], s[1], s[2])
+        _check(_on(self.device.index, _lib().fm_pages_append, self._pages_p, self._cache_p, rows, _ids(seqs, self.device, "seqs"),
                    _ids(row_off, self.device, "row_off"), _ids(path, self.device, "path") if path is not None else None, stride,
                    _ids(n_acc, self.device, "n_acc") if path is not None else None, n, max_rows), "fm_pages_append")
 
     def truncate(self, seqs, lens):
         """Cut sequences seqs[i] to at most lens[i] positions and give back the pages behind them (0: all)."""
         s, l, n = self._list(seqs, lens, "truncate")
-        _check(_on(self.device, _lib().fm_pages_truncate, self._pages_p, s, l, n), "fm_pages_truncate")
+        _check(_on(self.device.index, _lib().fm_pages_truncate, self._pages_p, s, l, n), "fm_pages_truncate")
 
     def compact(self):
         """Move the pages in use to the front of the pool; returns their number (int32 [1], on the device)."""
-        import torch
         used = torch.empty(1, dtype=torch.int32, device=self.device)
-        _check(_on(self.device, _lib().fm_pages_compact, self._pages_p, self._cache_p, used.data_ptr()), "fm_pages_compact")
+        _check(_on(self.device.index, _lib().fm_pages_compact, self._pages_p, self._cache_p, used.data_ptr()), "fm_pages_compact")
         return used
 
     def attention(self, layer, q, k_new, v_new, row_off, parent, seqs=None, window=0, n_prefix=0, scale=None, max_nodes=None, max_len=None,
@@ -205,7 +215,6 @@ class PagedCache:
         q [rows, heads, head_dim], k_new, v_new [rows, kv heads, head_dim] (rows may lie apart); row_off [n + 1]; parent [rows]: an earlier
         node of the tree, counted from its first row, or -1.  seqs [n]: the trees' sequences (None: 0 .. n-1).  max_nodes, max_len:
         bounds on a tree's nodes and a sequence's positions (default: what there is room for).  Returns out, or (out, lse)."""
-        import torch
         rows, heads, dh = q.shape if q.dim() == 3 else (0, 0, 0)
         n = row_off.numel() - 1
         _need(rows > 0 and q.stride(2) == 1 and q.stride(1) == dh == self.head_dim and q.dtype == self.dtype and q.device == self.device,
@@ -216,56 +225,62 @@ class PagedCache:
         _need(n >= 1 and parent.shape == (rows,) and (seqs is None and n <= self.max_seqs or seqs is not None and seqs.shape == (n,)),
               "attention: row_off [n + 1], parent [rows], seqs [n]")
         if out is None:
-            out = torch.empty((rows, heads, dh), dtype=q.dtype, device=self.device)
+            out = q.new_empty((rows, heads, dh))
         else:
             _need(out.shape == q.shape and out.dtype == q.dtype and out.device == self.device and out.stride(2) == 1 and out.stride(1) == dh, "attention: out like q")
         lse = torch.empty((rows, heads), dtype=torch.float32, device=self.device) if want_lse else None
-        room = self.max_pages * self.page_slots
-        # a single row has no distance to the next one that matters
-        apart = lambda t: t.stride(0) if rows > 1 else t.shape[1] * dh
-        a = FmTreeArgs(q.data_ptr(), k_new.data_ptr(), v_new.data_ptr(), out.data_ptr(), lse.data_ptr() if want_lse else None, apart(q), apart(k_new),
-                       apart(out), self._pages.table, self._pages.lens, _ids(seqs, self.device, "seqs") if seqs is not None else None,
-                       _ids(row_off, self.device, "row_off"), _ids(parent, self.device, "parent"), self._pages.status, self.max_pages, self.max_seqs, n,
-                       heads, min(rows, FM_MAX_TREE_NODES) if max_nodes is None else max_nodes, room if max_len is None else max_len, window, n_prefix,
-                       1.0 / math.sqrt(dh) if scale is None else scale)
-        lib = _lib()
-        size = lib.fm_tree_attention_bytes(self._cache_p, C.byref(a))
-        work = torch.empty(max(size, 1), dtype=torch.uint8, device=self.device)
-        _check(_on(self.device, lib.fm_tree_attention, self._cache_p, layer, C.byref(a), work.data_ptr(), size), "fm_tree_attention")
+        if max_nodes is None:
+            max_nodes = min(rows, FM_MAX_TREE_NODES)
+        # (a single row has no distance to the next one that matters)
+        q_row, new_row, out_row = (q.stride(0), k_new.stride(0), out.stride(0)) if rows > 1 else (heads * dh, self.n_kv_heads * dh, heads * dh)
+        p = self._pages
+        try:
+            a = _TREE.pack(q.data_ptr(), k_new.data_ptr(), v_new.data_ptr(), out.data_ptr(), lse.data_ptr() if want_lse else 0, q_row, new_row, out_row,
+                           p.table, p.lens, _ids(seqs, self.device, "seqs") if seqs is not None else 0, _ids(row_off, self.device, "row_off"),
+                           _ids(parent, self.device, "parent"), p.status, self.max_pages, self.max_seqs, n, heads, max_nodes,
+                           self.max_pages * self.page_slots if max_len is None else max_len, window, n_prefix, 1.0 / math.sqrt(dh) if scale is None else scale)
+        except (struct.error, OverflowError):
+            raise FmError(-1, "attention: a number out of range") from None
+        lib, size = _lib(), self._sizes.get((heads, max_nodes))
+        if size is None:
+            size = lib.fm_tree_attention_bytes(self._cache_p, a)     # (0 where the call itself will refuse)
+            if size:
+                self._sizes[heads, max_nodes] = size
+        work = torch.empty(size or 1, dtype=torch.uint8, device=self.device)
+        _check(_on(self.device.index, lib.fm_tree_attention, self._cache_p, layer, a, work.data_ptr(), size), "fm_tree_attention")
         return (out, lse) if want_lse else out
 
 
 def tree_accept(tokens, parent, row_off, predicted, max_nodes=None):
     """The longest path of every tree that the predictions confirm: (path [n, max_nodes] node indices, then -1; n_acc [n];
     next_token [n]).  tokens, parent, predicted [rows], row_off [n + 1]: int32 on the device."""
-    import torch
     device, n, rows = tokens.device, row_off.numel() - 1, tokens.numel()
     _need(tokens.is_cuda and tokens.dim() == 1 and parent.shape == predicted.shape == tokens.shape and n >= 1, "tree_accept: tokens, parent, predicted [rows]; row_off [n + 1]")
     stride = min(max(rows, 1), FM_MAX_TREE_NODES) if max_nodes is None else max_nodes
-    path = torch.empty((n, max(stride, 0)), dtype=torch.int32, device=device)
-    n_acc, nxt = (torch.empty(n, dtype=torch.int32, device=device) for _ in range(2))
-    _check(_on(device, _lib().fm_tree_accept, _ids(tokens, device, "tokens"), _ids(parent, device, "parent"), _ids(row_off, device, "row_off"),
+    path, n_acc, nxt = tokens.new_empty((n, max(stride, 0))), tokens.new_empty(n), tokens.new_empty(n)
+    _check(_on(device.index, _lib().fm_tree_accept, _ids(tokens, device, "tokens"), _ids(parent, device, "parent"), _ids(row_off, device, "row_off"),
                _ids(predicted, device, "predicted"), n, path.data_ptr(), stride, n_acc.data_ptr(), nxt.data_ptr()), "fm_tree_accept")
     return path, n_acc, nxt
+
+
+_SCORED = {torch.float32: FM_FP32, torch.bfloat16: FM_BF16, torch.float16: FM_FP16}
 
 
 def logprobs(logits, tokens=None, top=0):
     """Scores of logits rows [rows, vocab] (float32, bfloat16 or float16; rows may lie apart): (logprob [rows], entropy [rows], rank
     [rows], top_ids [rows, top], top_logprobs [rows, top]).  tokens: int32 [rows], or None (logprob -inf, rank -1)."""
-    import torch
-    types = {torch.float32: FM_FP32, torch.bfloat16: FM_BF16, torch.float16: FM_FP16}
-    _need(logits.dim() == 2 and logits.is_cuda and logits.dtype in types and logits.shape[1] >= 1 and (logits.stride(1) == 1 or logits.shape[1] == 1),
+    kind = _SCORED.get(logits.dtype)
+    _need(kind is not None and logits.dim() == 2 and logits.is_cuda and logits.shape[1] >= 1 and (logits.stride(1) == 1 or logits.shape[1] == 1),
           "logprobs: logits [rows, vocab] in float32, bfloat16 or float16 on a CUDA device")
     rows, vocab = logits.shape
     device = logits.device
-    _need(tokens is None or tokens.shape == (rows,), "logprobs: tokens [rows]")
-    _need(0 <= top <= vocab, "logprobs: top")
-    lp, ent = (torch.empty(rows, dtype=torch.float32, device=device) for _ in range(2))
-    rank = torch.empty(rows, dtype=torch.int32, device=device)
-    ids = torch.empty((rows, top), dtype=torch.int32, device=device)
-    tops = torch.empty((rows, top), dtype=torch.float32, device=device)
+    _need(0 <= top <= vocab and (tokens is None or tokens.shape == (rows,)), "logprobs: tokens [rows], top")
+    lp = torch.empty(rows, dtype=torch.float32, device=device)
+    ent, rank = torch.empty_like(lp), torch.empty_like(lp, dtype=torch.int32)
+    tops = lp.new_empty((rows, top))
+    ids = torch.empty_like(tops, dtype=torch.int32)
     if rows > 0:
-        _check(_on(device, _lib().fm_logprobs, logits.data_ptr(), types[logits.dtype], rows, vocab, logits.stride(0) if rows > 1 else vocab,
+        _check(_on(device.index, _lib().fm_logprobs, logits.data_ptr(), kind, rows, vocab, logits.stride(0) if rows > 1 else vocab,
                    _ids(tokens, device, "tokens") if tokens is not None else None, lp.data_ptr(), ent.data_ptr(), rank.data_ptr(), top, ids.data_ptr(),
                    tops.data_ptr()), "fm_logprobs")
     return lp, ent, rank, ids, tops

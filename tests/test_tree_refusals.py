@@ -40,7 +40,13 @@ def args(**kw):
     a = T.FmTreeArgs(P, P, P, P, None, 256, 128, 256, P, P, None, P, P, None, 5, 4, 2, 4, 8, 80, 0, 0, 0.125)
     for k, v in kw.items():
         setattr(a, k, v)
-    return a
+    return bytes(a)
+
+
+def test_packed_argument_blocks():
+    """The formats with which the binding packs them are those of the structures."""
+    n = list(range(1, 24))
+    assert T._TREE.pack(*n) == bytes(T.FmTreeArgs(*n)) and T._ROWS.pack(*n[:5]) == bytes(T.FmNewRows(*n[:5]))
 
 
 def test_work_sizes(lib):
@@ -53,7 +59,7 @@ def test_work_sizes(lib):
                                  dict(page_slots=0), dict(max_seqs=0), dict(max_seqs=5000), dict(max_pages=0)])
 def test_pages_refuse(lib, bad):
     p, c = pages(**bad), cache()
-    rows = T.FmNewRows(P, P, 0, 128, 64)
+    rows = bytes(T.FmNewRows(P, P, 0, 128, 64))
     assert lib.fm_pages_reset(p, None) == INVALID
     assert lib.fm_pages_fork(p, P, P, 1, None) == INVALID
     assert lib.fm_pages_truncate(p, P, P, 1, None) == INVALID
@@ -69,7 +75,7 @@ def test_page_lists_refuse(lib):
         assert call(None, P, 1) == INVALID and call(P, None, 1) == INVALID and call(P, P, -1) == INVALID
         assert call(P, P, T.FM_MAX_SEQS + 1) == CAPACITY and call(None, None, 0) == 0
     assert lib.fm_pages_reserve(p, c, P, P, 5, None) == INVALID          # more entries than sequences
-    append = lambda rows=rows, path=None, stride=0, acc=None, n=1, most=1: lib.fm_pages_append(p, c, rows, P, P, path, stride, acc, n, most, None)
+    append = lambda rows=rows, path=None, stride=0, acc=None, n=1, most=1: lib.fm_pages_append(p, c, bytes(rows), P, P, path, stride, acc, n, most, None)
     assert append(n=0) == 0
     for kw in (dict(path=P), dict(path=P, stride=4), dict(path=P, acc=P), dict(most=-1), dict(n=5), dict(rows=T.FmNewRows(None, P, 0, 128, 64)),
                dict(rows=T.FmNewRows(P + 8, P, 0, 128, 64)), dict(rows=T.FmNewRows(P, P, 4, 128, 64)), dict(rows=T.FmNewRows(P, P, 0, 127, 64)),
@@ -99,8 +105,8 @@ def test_a_table_of_too_many_positions(lib):
                                       (dict(n_heads=3), INVALID), (dict(max_nodes=0), INVALID), (dict(max_len=-1), INVALID), (dict(window=-1), INVALID),
                                       (dict(n_prefix=-1), INVALID), (dict(max_pages=0), INVALID), (dict(max_seqs=0), INVALID),
                                       (dict(q_row_stride=252), INVALID), (dict(q_row_stride=248), INVALID), (dict(new_row_stride=120), INVALID),
-                                      (dict(out_row_stride=248), INVALID), (dict(scale=float("nan")), INVALID), (dict(scale=float("inf")), INVALID),
-                                      (dict(batch=T.FM_MAX_SEQS + 1), CAPACITY), (dict(max_nodes=T.FM_MAX_TREE_NODES + 1), CAPACITY)])
+                                      (dict(out_row_stride=248), INVALID), (dict(scale=float("nan")), INVALID), (dict(scale=float("inf")), INVALID), (dict(scale=0.0), INVALID), (dict(scale=-1.0), INVALID),
+                                      (dict(batch=T.FM_MAX_TREES + 1), CAPACITY), (dict(max_nodes=T.FM_MAX_TREE_NODES + 1), CAPACITY)])
 def test_attention_refuses(lib, bad, code):
     assert lib.fm_tree_attention_bytes(cache(), args()) > 0
     assert lib.fm_tree_attention_bytes(cache(), args(**bad)) == 0
