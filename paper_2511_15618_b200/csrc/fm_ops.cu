@@ -158,23 +158,29 @@ bool make_maps(const fm_cache& c, int layer, int chunk, tr::Args& a) {
   return true;
 }
 
+// Will no tile be cut, whatever the lengths?  (See tr::make_plan: at most a tile per CTA, of eight chunks at most.)
+inline bool whole_for_sure(const tr::Args& a, int rows, int chunk, int ctas) {
+  const int64_t tiles = (int64_t)a.batch * a.Hkv * (((int64_t)a.max_nodes * a.G + rows - 1) / rows);
+  return tiles <= ctas && (a.max_len + chunk - 1) / chunk + 1 + (a.max_nodes + chunk - 1) / chunk <= 8;
+}
+
 template <typename T, int DH>
 int tree_attention(const tr::Args& a, cudaStream_t stream) {
-  cudaError_t e;
+  cudaError_t e = cudaSuccess;
   if (few_rows(a.max_nodes, a.G)) {
     static std::atomic<uint64_t> asked{0};
     using CF = tr::Rows16<DH>;
     if (!allow_smem(tr::rows16_kernel<T, DH>, CF::bytes(FM_MAX_TREES), asked)) return FM_ERR_CUDA;
     tr::rows16_kernel<T, DH><<<tr::SMS, CF::THREADS, CF::bytes(a.batch), stream>>>(a);
     if (cudaGetLastError() != cudaSuccess) return FM_ERR_CUDA;
-    e = launch_behind(tr::merge_kernel<T, DH, 16>, dim3(tr::SMS, 4), 256, stream, a);
+    if (!whole_for_sure(a, 16, CF::C, tr::SMS)) e = launch_behind(tr::merge_kernel<T, DH, 16>, dim3(tr::SMS, 4), 256, stream, a);
   } else {
     static std::atomic<uint64_t> asked{0};
     using CF = tr::Rows128<DH>;
     if (!allow_smem(tr::rows128_kernel<T, DH>, CF::bytes(FM_MAX_TREES), asked)) return FM_ERR_CUDA;
     tr::rows128_kernel<T, DH><<<2 * tr::SMS, CF::THREADS, CF::bytes(a.batch), stream>>>(a);
     if (cudaGetLastError() != cudaSuccess) return FM_ERR_CUDA;
-    e = launch_behind(tr::merge_kernel<T, DH, 128>, dim3(2 * tr::SMS, 8), 256, stream, a);
+    if (!whole_for_sure(a, 128, CF::C, 2 * tr::SMS)) e = launch_behind(tr::merge_kernel<T, DH, 128>, dim3(2 * tr::SMS, 8), 256, stream, a);
   }
   return e == cudaSuccess ? FM_OK : FM_ERR_CUDA;
 }

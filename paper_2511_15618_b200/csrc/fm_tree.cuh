@@ -258,48 +258,47 @@ __device__ inline int parts_of(const Args& a, const Plan& p, int cta, long long 
 }
 
 // ---- loading, by a warp
-// a chunk of cached positions as TMA boxes; every lane arrives on the barrier once
-template <typename T, int DH, int C>
-__device__ inline void request_boxes(const Args& a, const Seq& s, const Chunk& k, int hk, unsigned char* Ks, unsigned char* Vs, uint64_t* bar, int lane) {
-  constexpr int HALVES = DH / 64;
-  const int rows = min(a.page_div.d, C), boxes = (k.n + rows - 1) / rows;      // (at most C / 8 = 16)
-  int id = -1, in_page = 0;
-  if (lane < boxes) {
-    const int slot = k.start + lane * rows, pi = a.page_div(slot);
-    id = __ldg(a.table + (int64_t)s.seq * a.max_pages + pi);
-    in_page = slot - pi * a.page_div.d;
+// A chunk of cached positions as TMA boxes, a lane each.  The page id is read ahead of the wait for a place in the ring.
+// (Requests of a warp go out one after the other, some 75 ns each: several warps share a chunk's, one map or half each.)
+struct Box { int id, in_page; };                             // id -1: none
+template <int C>
+__device__ inline Box box_of(const Args& a, const Seq& s, const Chunk& k, int lane) {
+  const int rows = min(a.page_div.d, C), slot = k.start + lane * rows;         // (at most C / 8 = 16 boxes)
+  Box x{-1, 0};
+  if (!k.tree && lane * rows < k.n) {
+    const int pi = a.page_div(slot);
+    x.id = __ldg(a.table + (int64_t)s.seq * a.max_pages + pi);
+    x.in_page = slot - pi * a.page_div.d;
   }
-  const bool ok = id >= 0 && id < a.n_pages;
-  if (lane < boxes && !ok) {                                 // no page: zeros, and the caller is told
+  return x;
+}
+// boxes first, first + step, ... of 64 features from `x0` to `to` (rows of 128 bytes); every lane arrives on the barrier once
+template <int C>
+__device__ inline void request_boxes(const Args& a, const CUtensorMap* map, int x0, const Chunk& k, Box x, int first, int step, int hk, unsigned char* to,
+                                     uint64_t* bar, int lane) {
+  const int rows = min(a.page_div.d, C);
+  const bool mine = lane * rows < k.n && lane % step == first, ok = mine && x.id >= 0 && x.id < a.n_pages;
+  if (mine && !ok) {                                         // no page: zeros, and the caller is told
     if (a.status != nullptr) atomicMin(a.status, FM_ERR_INVALID_ARG);
-    for (int h = 0; h < HALVES; ++h)
-      for (int i = 0; i < rows * 8; ++i) {
-        reinterpret_cast<uint4*>(Ks + (h * C + lane * rows) * 128)[i] = make_uint4(0u, 0u, 0u, 0u);
-        reinterpret_cast<uint4*>(Vs + (h * C + lane * rows) * 128)[i] = make_uint4(0u, 0u, 0u, 0u);
-      }
+    for (int i = 0; i < rows * 8; ++i) reinterpret_cast<uint4*>(to + lane * rows * 128)[i] = make_uint4(0u, 0u, 0u, 0u);
     ptx::fence_proxy_async();
   }
   const int n = __popc(__ballot_sync(0xffffffffu, ok));
-  if (lane == 0) ptx::mbar_expect_tx(bar, (uint32_t)(n * rows * 128 * 2 * HALVES)); else ptx::mbar_arrive(bar);
+  if (lane == 0) ptx::mbar_expect_tx(bar, (uint32_t)(n * rows * 128)); else ptx::mbar_arrive(bar);
   __syncwarp();
-  if (ok) {
-#pragma unroll
-    for (int h = 0; h < HALVES; ++h) {
-      ptx::tma_load_4d(Ks + (h * C + lane * rows) * 128, &a.map_k, h * 64, in_page, hk, id, bar);
-      ptx::tma_load_4d(Vs + (h * C + lane * rows) * 128, &a.map_v, h * 64, in_page, hk, id, bar);
-    }
-  }
+  if (ok) ptx::tma_load_4d(to + lane * rows * 128, map, x0, x.in_page, hk, x.id, bar);
   __syncwarp();
 }
-// the same with 16-byte copies, also for nodes; what is not there is zero.  The copies are the calling threads' (cp.async).
-template <typename T, int DH, int C>
-__device__ inline void request_pieces(const Args& a, const Seq& s, const Chunk& k, int hk, unsigned char* Ks, unsigned char* Vs, int lane) {
-  constexpr int PIECES = DH / 8, STEP = 32 / PIECES;
-  const int piece = lane % PIECES;
+// The same with 16-byte copies, also for nodes; what is not there is zero.  By `threads` threads, the calling one is `t`;
+// the copies are theirs (cp.async).  KV: 0 keys, 1 values, 2 both.
+template <typename T, int DH, int C, int KV>
+__device__ inline void request_pieces(const Args& a, const Seq& s, const Chunk& k, int hk, unsigned char* Ks, unsigned char* Vs, int t, int threads) {
+  constexpr int PIECES = DH / 8;
+  const int piece = t % PIECES, step = threads / PIECES;
   const uint32_t ks = ptx::smem_u32(Ks) + (piece >> 3) * C * 128, vs = ptx::smem_u32(Vs) + (piece >> 3) * C * 128;
   const int* table = a.table + (int64_t)s.seq * a.max_pages;
 #pragma unroll 4
-  for (int r = lane / PIECES; r < C; r += STEP) {
+  for (int r = t / PIECES; r < C; r += step) {
     bool there = r < k.n;
     const T *kp = reinterpret_cast<const T*>(a.k), *vp = reinterpret_cast<const T*>(a.v);
     int64_t at = 0;
@@ -316,18 +315,18 @@ __device__ inline void request_pieces(const Args& a, const Seq& s, const Chunk& 
       }
     }
     const uint32_t to = ptx::swz128(r, piece & 7);
-    cp16(ks + to, kp + at + piece * 8, there);
-    cp16(vs + to, vp + at + piece * 8, there);
+    if (KV != 1) cp16(ks + to, kp + at + piece * 8, there);
+    if (KV != 0) cp16(vs + to, vp + at + piece * 8, there);
   }
 }
 // query rows of a tile, behind the last one zeros; halves of ROWS x 128 bytes
 template <typename T, int DH, int ROWS>
-__device__ inline void request_queries(const Args& a, const Seq& s, int hk, int mt, unsigned char* Q, int lane) {
-  constexpr int PIECES = DH / 8, STEP = 32 / PIECES;
-  const int piece = lane % PIECES, M = s.n * a.G;
+__device__ inline void request_queries(const Args& a, const Seq& s, int hk, int mt, unsigned char* Q, int t, int threads) {
+  constexpr int PIECES = DH / 8;
+  const int piece = t % PIECES, M = s.n * a.G, step = threads / PIECES;
   const uint32_t qs = ptx::smem_u32(Q) + (piece >> 3) * ROWS * 128;
 #pragma unroll 4
-  for (int r = lane / PIECES; r < ROWS; r += STEP) {
+  for (int r = t / PIECES; r < ROWS; r += step) {
     const int idx = mt * ROWS + r;
     const bool there = idx < M;
     const int node = there ? idx / a.G : 0, gh = there ? idx - node * a.G : 0;
@@ -412,13 +411,13 @@ __device__ inline void build_tree(Tree& t, const int* parent, int n, int tid, Sy
 // sixteen query rows a tile, warp-level MMAs
 // ------------------------------------------------------------------------------------------
 // Eight warps multiply: four take the even chunks, four the odd ones, each a fixed slice of a chunk with its own running maximum,
-// sum and output (base 2); their states are merged at the end of a tile.  One warp loads, queries of the next tile included.
+// sum and output (base 2); their states are merged at the end of a tile.  Four warps load, queries of the next tile included.
 template <int DH>
 struct Rows16 {
   static constexpr int ROWS = 16, C = DH == 64 ? 128 : 64, NW = 4, KPW = C / NW, STAGES = 4;
   static constexpr int TILE = C * DH * 2, STAGE = 2 * TILE, RING = STAGES * STAGE, Q = 16 * DH * 2;
   static constexpr int STATES = NW * 16 * (DH + 2) * 4;
-  static constexpr int THREADS = 2 * NW * 32 + 32;
+  static constexpr int THREADS = 2 * NW * 32 + 128;
   static constexpr int FIXED = RING + 2 * Q + STATES + (int)sizeof(Tree) + 1024 + 512;
   static int bytes(int batch) { return FIXED + plan_bytes(batch); }
 };
@@ -435,7 +434,7 @@ __global__ void __launch_bounds__(Rows16<DH>::THREADS, 1) rows16_kernel(const __
   int4* s_info = reinterpret_cast<int4*>(pw + NW * 16 * (DH + 2));
   long long* s_base = reinterpret_cast<long long*>(s_info + a.batch);
   long long* s_sh = s_base + a.batch + 1;                    // [2 * warps]
-  uint64_t* full = reinterpret_cast<uint64_t*>(s_sh + 20);
+  uint64_t* full = reinterpret_cast<uint64_t*>(s_sh + 24);
   uint64_t *empty = full + ST, *q_full = empty + ST, *q_free = q_full + 2;
   Tree& tree = *reinterpret_cast<Tree*>(q_free + 2);
   int* s_tile_base = reinterpret_cast<int*>(&tree + 1);
@@ -444,8 +443,8 @@ __global__ void __launch_bounds__(Rows16<DH>::THREADS, 1) rows16_kernel(const __
   ptx::grid_dep_launch();
   if (threadIdx.x == 0) {
     s_fail = s_stop = 0;
-    for (int i = 0; i < ST; ++i) { ptx::mbar_init(full + i, 32); ptx::mbar_init(empty + i, NW); }
-    for (int i = 0; i < 2; ++i) { ptx::mbar_init(q_full + i, 32); ptx::mbar_init(q_free + i, 2 * NW); }
+    for (int i = 0; i < ST; ++i) { ptx::mbar_init(full + i, 128); ptx::mbar_init(empty + i, NW); }
+    for (int i = 0; i < 2; ++i) { ptx::mbar_init(q_full + i, 128); ptx::mbar_init(q_free + i, 2 * NW); }
     ptx::fence_mbar_init();
   }
   Plan plan;
@@ -455,8 +454,12 @@ __global__ void __launch_bounds__(Rows16<DH>::THREADS, 1) rows16_kernel(const __
   auto wait = [](uint64_t* bar, uint32_t parity) { return __all_sync(0xffffffffu, ptx::mbar_wait(bar, parity)) != 0; };
   __syncthreads();
 
-  if (warp == 2 * NW) {
-    // ---- loading
+  if (warp >= 2 * NW) {
+    // ---- loading: warps 0 and 2 keys, 1 and 3 values; of 128 features half each, of 64 every other box
+    const int lw = warp - 2 * NW, tid = threadIdx.x - 2 * NW * 32;
+    const CUtensorMap* map = (lw & 1) ? &a.map_v : &a.map_k;
+    const int x0 = DH == 128 ? (lw >> 1) * 64 : 0, first = DH == 128 ? 0 : lw >> 1, step = DH == 128 ? 1 : 2;
+    const int off = (lw & 1) * CF::TILE + (DH == 128 ? (lw >> 1) * C * 128 : 0);
     int i = 0, part = 0, written = 0;                        // chunks left whose place threads have written
     int4 cut = make_int4(0, 0, 0, 0);
     long long cut_end = 0;
@@ -465,26 +468,28 @@ __global__ void __launch_bounds__(Rows16<DH>::THREADS, 1) rows16_kernel(const __
       const int hk = w.tile / w.s.tiles, mt = w.tile - hk * w.s.tiles;
       if (w.starts() && !w.ends()) { cut = make_int4(w.b, hk, mt, 1); cut_end = w.tile_start + w.s.chunks + OVER; }
       if (part >= 2 && !(ok = wait(q_free + (part & 1), ((part >> 1) - 1) & 1))) break;
-      request_queries<T, DH, 16>(a, w.s, hk, mt, sq + (part & 1) * CF::Q, lane);
+      request_queries<T, DH, 16>(a, w.s, hk, mt, sq + (part & 1) * CF::Q, tid, 128);
       cp_arrive(q_full + (part & 1));
       ++part;
+      Chunk k = chunk_of<C>(w.s, w.c);
+      Box x = box_of<C>(a, w.s, k, lane);
       for (int c = w.c; c < w.c_end; ++c, ++i) {
-        const Chunk k = chunk_of<C>(w.s, c);
         const int st = i % ST;
         if (i >= ST && !(ok = wait(empty + st, ((i / ST) - 1) & 1))) break;
         unsigned char* Ks = sm + st * CF::STAGE;
         if (a.tma && !k.tree) {
           if (written > 0) { --written; ptx::fence_proxy_async(); }
-          request_boxes<T, DH, C>(a, w.s, k, hk, Ks, Ks + CF::TILE, full + st, lane);
+          request_boxes<C>(a, map, x0, k, x, first, step, hk, Ks + off, full + st, lane);
         } else {
-          request_pieces<T, DH, C>(a, w.s, k, hk, Ks, Ks + CF::TILE, lane);
+          request_pieces<T, DH, C, 2>(a, w.s, k, hk, Ks, Ks + CF::TILE, tid, 128);
           cp_arrive(full + st);
           written = ST;
         }
+        if (c + 1 < w.c_end) { k = chunk_of<C>(w.s, c + 1); x = box_of<C>(a, w.s, k, lane); }
       }
     }
     if (!ok) s_fail = 1;
-    write_desc<C, 16>(a, plan, cut, cut_end, lane);
+    if (lw == 0) write_desc<C, 16>(a, plan, cut, cut_end, lane);
     asm volatile("cp.async.wait_all;" ::: "memory");
   } else {
     // ---- multiplying
@@ -738,13 +743,14 @@ __global__ void __launch_bounds__(Rows16<DH>::THREADS, 1) rows16_kernel(const __
 // MN-major), P goes back to tensor memory as the A operand.  Two threads share a row of the softmax and exchange
 // maxima; S of the next chunk is multiplied as soon as S is in registers.  The output is rescaled only when a row's
 // maximum has grown by more than 2^8 (P then stays below 2^8).  Two CTAs per SM: one's softmax
-// runs under the other's MMAs.  One warp requests the chunks' boxes.  A second one (the fixer) brings what boxes do not: queries,
-// nodes, odd pages; it takes values that are not finite out of chunks with hidden keys, and makes its writes visible to
-// the tensor cores by a proxy fence.
+// runs under the other's MMAs.  One warp brings keys, one values, each as soon as its place is free (keys once their scores
+// are multiplied); a third one (the fixer) brings queries and takes values that are not finite out of chunks with hidden keys.  What
+// threads write is made visible to the tensor cores by a proxy fence.  P has two places: the exponentials of a chunk do
+// not wait for the product of the one before.
 template <int DH>
 struct Rows128 {
   static constexpr int ROWS = 128, C = 64, STAGES = DH == 64 ? 4 : 2, HC = C / 2;
-  static constexpr int THREADS = 64 + 32 + 256;
+  static constexpr int THREADS = 96 + 256 + 32;              // keys, fixer, MMA, softmax, values
   static constexpr int Q = 128 * DH * 2, TILE = C * DH * 2, STAGE = 2 * TILE;
   static constexpr int FIXED = Q + STAGES * STAGE + (int)sizeof(Tree) + 512 * 4 + 512 + 1024;
   static int bytes(int batch) { return FIXED + plan_bytes(batch); }
@@ -835,8 +841,8 @@ __global__ void __launch_bounds__(Rows128<DH>::THREADS, 2) rows128_kernel(const 
   long long* s_base = reinterpret_cast<long long*>(s_info + a.batch);
   long long* s_sh = s_base + a.batch + 1;                    // [2 * warps]
   uint64_t* full = reinterpret_cast<uint64_t*>(s_sh + 24);
-  uint64_t *fixed = full + ST, *empty = fixed + ST, *q_full = empty + ST, *q_free = q_full + 1, *s_full = q_free + 1, *s_read = s_full + 1, *p_full = s_read + 1,
-           *o_full = p_full + 1, *done = o_full + 1;
+  uint64_t *full_v = full + ST, *fixed = full_v + ST, *free_k = fixed + ST, *free_v = free_k + ST, *q_full = free_v + ST, *q_free = q_full + 1, *s_full = q_free + 1, *s_read = s_full + 1, *p_full = s_read + 1,
+           *o_full = p_full + 2, *done = o_full + 2;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(done + 1);
   Tree& tree = *reinterpret_cast<Tree*>(done + 2);
   int* s_tile_base = reinterpret_cast<int*>(&tree + 1);
@@ -845,9 +851,12 @@ __global__ void __launch_bounds__(Rows128<DH>::THREADS, 2) rows128_kernel(const 
   ptx::grid_dep_launch();
   if (threadIdx.x == 0) {
     s_fail = s_bad = 0;
-    for (int i = 0; i < ST; ++i) { ptx::mbar_init(full + i, 32); ptx::mbar_init(fixed + i, 32); ptx::mbar_init(empty + i, 1); }
-    ptx::mbar_init(q_full, 32); ptx::mbar_init(q_free, 1); ptx::mbar_init(s_full, 1); ptx::mbar_init(s_read, 8); ptx::mbar_init(p_full, 8);
-    ptx::mbar_init(o_full, 1); ptx::mbar_init(done, 1);
+    for (int i = 0; i < ST; ++i) {
+      ptx::mbar_init(full + i, 32); ptx::mbar_init(full_v + i, 32); ptx::mbar_init(fixed + i, 32);
+      ptx::mbar_init(free_k + i, 1); ptx::mbar_init(free_v + i, 1);
+    }
+    ptx::mbar_init(q_full, 32); ptx::mbar_init(q_free, 1); ptx::mbar_init(s_full, 1); ptx::mbar_init(s_read, 8); ptx::mbar_init(p_full, 8); ptx::mbar_init(p_full + 1, 8);
+    ptx::mbar_init(o_full, 1); ptx::mbar_init(o_full + 1, 1); ptx::mbar_init(done, 1);
     ptx::fence_mbar_init();
   }
   if (warp == 2) {
@@ -861,11 +870,13 @@ __global__ void __launch_bounds__(Rows128<DH>::THREADS, 2) rows128_kernel(const 
   tc::fence_before();
   __syncthreads();
   tc::fence_after();
-  const uint32_t tmem = ptx::uniform(*tmem_slot), tO = tmem + C, tP = tO + DH;             // S in columns 0 .. C-1, then O, then P
+  const uint32_t tmem = ptx::uniform(*tmem_slot), tO = tmem + C, tP = tO + DH;             // S in columns 0 .. C-1, then O, then P twice
   auto wait = [](uint64_t* bar, uint32_t parity) { return __all_sync(0xffffffffu, ptx::mbar_wait(bar, parity)) != 0; };
 
-  if (warp == 0) {
-    // ---- requesting
+  if (warp == 0 || warp == 11) {
+    // ---- keys, values
+    const bool v = warp == 11;
+    uint64_t *mine = v ? full_v : full, *room = v ? free_v : free_k;
     int i = 0;
     int4 cut = make_int4(0, 0, 0, 0);
     long long cut_end = 0;
@@ -873,16 +884,43 @@ __global__ void __launch_bounds__(Rows128<DH>::THREADS, 2) rows128_kernel(const 
     while (ok && w.next(a, plan)) {
       const int hk = w.tile / w.s.tiles;
       if (w.starts() && !w.ends()) { cut = make_int4(w.b, hk, w.tile - hk * w.s.tiles, 1); cut_end = w.tile_start + w.s.chunks + OVER; }
+      Chunk k = chunk_of<C>(w.s, w.c);
+      Box x = box_of<C>(a, w.s, k, lane);
       for (int c = w.c; c < w.c_end; ++c, ++i) {
-        const Chunk k = chunk_of<C>(w.s, c);
         const int st = i % ST;
-        if (i >= ST && !(ok = wait(empty + st, ((i / ST) - 1) & 1))) break;
-        if (a.tma && !k.tree) request_boxes<T, DH, C>(a, w.s, k, hk, ring + st * STAGE, ring + st * STAGE + TILE, full + st, lane);
-        else ptx::mbar_arrive(full + st);                    // the fixer brings it
+        unsigned char *Ks = ring + st * STAGE, *Vs = Ks + TILE;
+        if (i >= ST && !(ok = wait(room + st, ((i / ST) - 1) & 1))) break;
+        if (a.tma && !k.tree) {
+          // (both halves of a box in a lane: they land on one barrier, which every lane arrives on once)
+          const CUtensorMap* map = v ? &a.map_v : &a.map_k;
+          const int rows = min(a.page_div.d, C);
+          const bool has = lane * rows < k.n, good = has && x.id >= 0 && x.id < a.n_pages;
+          unsigned char* to = (v ? Vs : Ks) + lane * rows * 128;
+          if (has && !good) {                                // no page: zeros, and the caller is told
+            if (a.status != nullptr) atomicMin(a.status, FM_ERR_INVALID_ARG);
+            for (int h = 0; h < DH / 64; ++h)
+              for (int j = 0; j < rows * 8; ++j) reinterpret_cast<uint4*>(to + h * C * 128)[j] = make_uint4(0u, 0u, 0u, 0u);
+            ptx::fence_proxy_async();
+          }
+          const int n = __popc(__ballot_sync(0xffffffffu, good));
+          if (lane == 0) ptx::mbar_expect_tx(mine + st, (uint32_t)(n * rows * 128 * (DH / 64))); else ptx::mbar_arrive(mine + st);
+          __syncwarp();
+          if (good) {
+#pragma unroll
+            for (int h = 0; h < DH / 64; ++h) ptx::tma_load_4d(to + h * C * 128, map, h * 64, x.in_page, hk, x.id, mine + st);
+          }
+          __syncwarp();
+        } else {
+          if (v) request_pieces<T, DH, C, 1>(a, w.s, k, hk, Ks, Vs, lane, 32); else request_pieces<T, DH, C, 0>(a, w.s, k, hk, Ks, Vs, lane, 32);
+          asm volatile("cp.async.wait_all;" ::: "memory");
+          ptx::fence_proxy_async();
+          ptx::mbar_arrive(mine + st);
+        }
+        if (c + 1 < w.c_end) { k = chunk_of<C>(w.s, c + 1); x = box_of<C>(a, w.s, k, lane); }
       }
     }
     if (!ok) s_fail = 1;
-    write_desc<C, 128>(a, plan, cut, cut_end, lane);
+    if (!v) write_desc<C, 128>(a, plan, cut, cut_end, lane);
   } else if (warp == 1) {
     // ---- fixing
     int i = 0, part = 0;
@@ -891,7 +929,7 @@ __global__ void __launch_bounds__(Rows128<DH>::THREADS, 2) rows128_kernel(const 
       const int hk = w.tile / w.s.tiles;
       // the tile's queries, once the scores of the tile before have been multiplied
       if (part > 0 && !(ok = wait(q_free, (part - 1) & 1))) break;
-      request_queries<T, DH, 128>(a, w.s, hk, w.tile - hk * w.s.tiles, sm, lane);
+      request_queries<T, DH, 128>(a, w.s, hk, w.tile - hk * w.s.tiles, sm, lane, 32);
       asm volatile("cp.async.wait_all;" ::: "memory");
       ptx::fence_proxy_async();
       ptx::mbar_arrive(q_full);
@@ -899,27 +937,20 @@ __global__ void __launch_bounds__(Rows128<DH>::THREADS, 2) rows128_kernel(const 
       for (int c = w.c; c < w.c_end; ++c, ++i) {
         const Chunk k = chunk_of<C>(w.s, c);
         const int st = i % ST;
-        unsigned char* Vs = ring + st * STAGE + TILE;
-        if (i >= ST && !(ok = wait(empty + st, ((i / ST) - 1) & 1))) break;
-        const bool uneven = uneven_chunk<C>(a, w.s, k);
-        if (k.tree || !a.tma) {
-          request_pieces<T, DH, C>(a, w.s, k, hk, ring + st * STAGE, Vs, lane);
-          asm volatile("cp.async.wait_all;" ::: "memory");
-          __syncwarp();
-        } else if (uneven) {
-          if (!(ok = wait(full + st, (i / ST) & 1))) break;
-        }
-        if (uneven) {
+        // (for every chunk: this warp must not fall two phases behind a barrier, a parity tells two apart, nor run ahead)
+        if (!(ok = wait(full_v + st, (i / ST) & 1))) break;
+        if (uneven_chunk<C>(a, w.s, k)) {
+          uint4* Vs = reinterpret_cast<uint4*>(ring + st * STAGE + TILE);
           bool bad = false;
           for (int j = lane; j < TILE / 16; j += 32) {
-            uint4 v = reinterpret_cast<uint4*>(Vs)[j];
+            uint4 u = Vs[j];
             bool here = false;
-            v.x = finite_part<T>(v.x, here); v.y = finite_part<T>(v.y, here); v.z = finite_part<T>(v.z, here); v.w = finite_part<T>(v.w, here);
-            if (here) { reinterpret_cast<uint4*>(Vs)[j] = v; bad = true; }
+            u.x = finite_part<T>(u.x, here); u.y = finite_part<T>(u.y, here); u.z = finite_part<T>(u.z, here); u.w = finite_part<T>(u.w, here);
+            if (here) { Vs[j] = u; bad = true; }
           }
           if (bad) *reinterpret_cast<volatile int*>(&s_bad) = 1;
+          ptx::fence_proxy_async();
         }
-        if (uneven || !a.tma) ptx::fence_proxy_async();
         ptx::mbar_arrive(fixed + st);
       }
     }
@@ -935,7 +966,7 @@ __global__ void __launch_bounds__(Rows128<DH>::THREADS, 2) rows128_kernel(const 
     auto scores = [&](int i, bool first, bool last) {
       const int st = i % ST;
       if (first && !wait(q_full, part++ & 1)) return false;
-      if (!wait(full + st, (i / ST) & 1) || !wait(fixed + st, (i / ST) & 1)) return false;
+      if (!wait(full + st, (i / ST) & 1)) return false;
       tc::fence_after();
       const uint64_t dk = tc::smem_desc_sw128(ptx::smem_u32(ring + st * STAGE));
       if (ptx::elect_one()) {
@@ -943,6 +974,7 @@ __global__ void __launch_bounds__(Rows128<DH>::THREADS, 2) rows128_kernel(const 
         for (int k = 0; k < DH / 16; ++k)                    // 64 features a half, 16 a step
           tc::mma_ss(tmem, dq + (k >> 2) * (128 * 128 / 16) + 2 * (k & 3), dk + (k >> 2) * (C * 128 / 16) + 2 * (k & 3), id_s, k > 0 ? 1u : 0u);
         tc::commit(s_full);
+        tc::commit(free_k + st);
         if (last) tc::commit(q_free);
       }
       return true;
@@ -956,16 +988,16 @@ __global__ void __launch_bounds__(Rows128<DH>::THREADS, 2) rows128_kernel(const 
       if (!(ok = wait(s_read, it & 1))) break;
       if (last) { more = w.next(a, plan); c = w.c; } else { ++c; }
       if (more && !(ok = scores(it + 1, last, c + 1 == w.c_end))) break;
-      if (!(ok = wait(p_full, it & 1))) break;
+      if (!(ok = wait(full_v + st, (it / ST) & 1) && wait(fixed + st, (it / ST) & 1) && wait(p_full + (it & 1), (it >> 1) & 1))) break;
       tc::fence_after();
       const uint64_t dv = tc::smem_desc_sw128(ptx::smem_u32(ring + st * STAGE + TILE));
       if (ptx::elect_one()) {
 #pragma unroll
         for (int h = 0; h < DH / 64; ++h)
 #pragma unroll
-          for (int k = 0; k < C / 16; ++k) mma_ts(tO + 64 * h, tP + 8 * k, dv + h * (C * 128 / 16) + 128 * k, id_o, (!first || k > 0) ? 1u : 0u);
-        tc::commit(empty + st);
-        tc::commit(o_full);
+          for (int k = 0; k < C / 16; ++k) mma_ts(tO + 64 * h, tP + 32 * (it & 1) + 8 * k, dv + h * (C * 128 / 16) + 128 * k, id_o, (!first || k > 0) ? 1u : 0u);
+        tc::commit(free_v + st);
+        tc::commit(o_full + (it & 1));
       }
       ++it;
     }
@@ -1031,15 +1063,17 @@ __global__ void __launch_bounds__(Rows128<DH>::THREADS, 2) rows128_kernel(const 
         pair[half * 128 + i_row] = mx;
         meet();
         mx = fmaxf(mx, pair[(half ^ 1) * 128 + i_row]);
-        // P of the chunk before has been multiplied: its place, and O, are free
-        if (!first) ok = ok && wait(o_full, (it - 1) & 1);
+        // P of the chunk two before has been multiplied: its place is free (behind the first chunks of the launch)
+        if (it >= 2) ok = ok && wait(o_full + (it & 1), ((it >> 1) - 1) & 1);
         tc::fence_after();
         const bool grow = mx > m + GROW || (m == -INFINITY && mx != -INFINITY);
         if (__any_sync(0xffffffffu, grow)) {
           const float mn = grow ? mx : m, f = m == -INFINITY ? (grow ? 0.f : 1.f) : ex2(m - mn);
           m = mn;
           l *= f;
-          if (!first) {                                      // this half's columns of the output
+          if (!first) {                                      // this half's columns of the output, once the chunk before is in
+            ok = ok && wait(o_full + ((it - 1) & 1), ((it - 1) >> 1) & 1);
+            tc::fence_after();
 #pragma unroll 1
             for (int j = 0; j < DH / 2; j += 16) {
               uint32_t o[16];
@@ -1063,20 +1097,20 @@ __global__ void __launch_bounds__(Rows128<DH>::THREADS, 2) rows128_kernel(const 
             sum[k & 1] = add2(sum[k & 1], pack2(e0, e1));
             pk[k] = pack(e0, e1, T());
           }
-          st16(tP + lanes + (HC * half + j) / 2, pk);
+          st16(tP + 32 * (it & 1) + lanes + (HC * half + j) / 2, pk);
         }
         const float2 sa = unpack2(sum[0]), sb = unpack2(sum[1]);
         l += (sa.x + sa.y) + (sb.x + sb.y);
         st_wait();
         tc::fence_before();
         __syncwarp();
-        if (lane == 0) ptx::mbar_arrive(p_full);
+        if (lane == 0) ptx::mbar_arrive(p_full + (it & 1));
       }
       float* pair = s_pair + (x++ & 1) * 256;
       pair[half * 128 + i_row] = l;
       meet();
       l += pair[(half ^ 1) * 128 + i_row];
-      ok = ok && wait(o_full, (it - 1) & 1);
+      ok = ok && wait(o_full + ((it - 1) & 1), ((it - 1) >> 1) & 1);
       tc::fence_after();
       const bool live = there && tree.reach[node][node >> 5] != 0u;
       const float inv = live ? 1.f / l : 0.f;
@@ -1141,18 +1175,20 @@ __global__ void __launch_bounds__(Rows128<DH>::THREADS, 2) rows128_kernel(const 
   if (warp == 2) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(256) : "memory");
 }
 
-// ---- parts of the tiles that were cut, merged in order: grid (CTAs, blocks per tile), two warps a row, four rows at a time
+// ---- parts of the tiles that were cut, merged in order: grid (CTAs, blocks per tile); two, four or eight warps a row, by the number of
+// parts (one tile over all SMs has 148: two warps a row took 20 us for them)
 template <typename T, int DH, int ROWS>
 __global__ void __launch_bounds__(256) merge_kernel(const __grid_constant__ Args a) {
   constexpr int CL = DH / 32, GS = ROWS * (DH + 2);
-  __shared__ float s_o[4][DH];
-  __shared__ float2 s_ml[4];
+  __shared__ float s_o[8][DH];
+  __shared__ float2 s_ml[8];
   ptx::grid_dep_wait();
   const int4 d = __ldcg(a.desc + blockIdx.x);
   if (d.w < 2) return;
   const int r0 = a.row_off[d.x], n = min(a.row_off[d.x + 1] - r0, a.max_nodes), rows = min(ROWS, n * a.G - d.z * ROWS);
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, r = warp & 3, half = warp >> 2;
-  for (int i0 = blockIdx.y * 4; i0 < rows; i0 += gridDim.y * 4) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int wpr = d.w <= 8 ? 2 : (d.w <= 32 ? 4 : 8), rpb = 8 / wpr, r = warp / wpr, q = warp - r * wpr;     // warps a row, rows a round
+  for (int i0 = blockIdx.y * rpb; i0 < rows; i0 += gridDim.y * rpb) {
     const int i = i0 + r, idx = d.z * ROWS + i;
     const bool there = i < rows;
     float m = -INFINITY, l = 0.f, o[CL];
@@ -1168,13 +1204,14 @@ __global__ void __launch_bounds__(256) merge_kernel(const __grid_constant__ Args
     };
     if (there) {
       constexpr int U = 4;
-      for (int k0 = half; k0 < d.w; k0 += 2 * U) {
+      const int per = (d.w + wpr - 1) / wpr, k1 = min(d.w, (q + 1) * per);     // neighbouring parts a warp
+      for (int k0 = q * per; k0 < k1; k0 += U) {
         float2 ml[U];
         float v[U][CL];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-          const int k = k0 + 2 * u;
-          if (k >= d.w) continue;
+          const int k = k0 + u;
+          if (k >= k1) continue;
           const float* row = a.part + ((size_t)(blockIdx.x + k) * 2 + (k == 0 ? 1 : 0)) * GS + (size_t)i * (DH + 2);
           ml[u] = __ldcg(reinterpret_cast<const float2*>(row + DH));
 #pragma unroll
@@ -1182,21 +1219,23 @@ __global__ void __launch_bounds__(256) merge_kernel(const __grid_constant__ Args
         }
 #pragma unroll
         for (int u = 0; u < U; ++u)
-          if (k0 + 2 * u < d.w) add(ml[u].x, ml[u].y, v[u]);
+          if (k0 + u < k1) add(ml[u].x, ml[u].y, v[u]);
       }
     }
     __syncthreads();                                         // (the rows before have been read)
-    if (half == 1) {
+    if (q != 0) {
 #pragma unroll
-      for (int j = 0; j < CL; ++j) s_o[r][lane + 32 * j] = o[j];
-      if (lane == 0) s_ml[r] = make_float2(m, l);
+      for (int j = 0; j < CL; ++j) s_o[warp][lane + 32 * j] = o[j];
+      if (lane == 0) s_ml[warp] = make_float2(m, l);
     }
     __syncthreads();
-    if (half == 1 || !there) continue;
-    float o2[CL];
+    if (q != 0 || !there) continue;
+    for (int k = 1; k < wpr; ++k) {
+      float o2[CL];
 #pragma unroll
-    for (int j = 0; j < CL; ++j) o2[j] = s_o[r][lane + 32 * j];
-    add(s_ml[r].x, s_ml[r].y, o2);
+      for (int j = 0; j < CL; ++j) o2[j] = s_o[warp + k][lane + 32 * j];
+      add(s_ml[warp + k].x, s_ml[warp + k].y, o2);
+    }
     const int nd = idx / a.G, gh = idx - nd * a.G, h = d.y * a.G + gh;
     const bool live = !(m == -INFINITY && l == 0.f);         // (a node in use sees itself)
     const float inv = live ? 1.f / l : 0.f;
