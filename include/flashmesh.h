@@ -300,6 +300,28 @@ int fm_verify_static_scratch(fm_ctx* ctx, const int32_t* cand /*DEV*/, int32_t* 
 int fm_accept(fm_ctx* ctx, const int32_t* force_len /*DEV*/, const int32_t* force_tok /*DEV*/,
               int32_t* n_acc /*DEV*/, int32_t* emitted /*DEV*/, int32_t* kv_len /*DEV*/);
 
+/* Verify a tree of candidates instead of one chain: several alternatives per position, for instance the top
+ * alternatives of the draft distributions (fm_logprobs on fm_draft's logits).  tokens, parent: DEV
+ * int32 [batch, nodes], nodes <= D+1.  Node 0 of a sequence is the pending main token (parent -1); another node continues
+ * the earlier node of its sequence that parent names; a node whose parent is none, or deeper than the rows a pass
+ * would feed, is not in use.  A node at depth k stands for position L + k and sees the accepted positions and its
+ * ancestors, through all level stacks (fm_tree_attention over the context's caches).  predicted: DEV
+ * int32 out [batch, nodes] (masked argmax, -1 where not in use) or NULL; logits: DEV float32 out
+ * [batch, nodes, V] or NULL; margin: DEV float32 out [batch, nodes] or NULL.  Changes no cache entry and
+ * does not move L; calling it twice is legal.  Its projections run in the tiled form, as a prefill's: a chain verified as a tree
+ * agrees with fm_verify to rounding, not to the bit (see the statement on lossless decoding above).
+ * Errors: INVALID_ARG, BAD_STATE (before fm_prefill), CAPACITY (nodes > D+1, or more rows than a prefill chunk's faces). */
+int fm_verify_tree(fm_ctx* ctx, const int32_t* tokens /*DEV*/, const int32_t* parent /*DEV*/, int32_t nodes, int32_t* predicted /*DEV*/,
+                   float* logits /*DEV*/, float* margin /*DEV*/);
+
+/* Accept the longest confirmed path of the tree (fm_tree_accept on the predictions; it ends at an accepted EOS) and move its keys,
+ * values and carried hiddens into the caches; L += its length; the next main token is the prediction at its last node.
+ * force_pred: DEV int32 [batch, nodes] or NULL, replaces the stored predictions.  path: DEV int32 out
+ * [batch, nodes], node indices, then -1; emitted: DEV int32 out [batch, nodes], their tokens, then -1; n_acc, kv_len as
+ * in fm_accept.  Any output may be NULL.  Errors: BAD_STATE if no fm_verify_tree preceded it. */
+int fm_accept_tree(fm_ctx* ctx, const int32_t* force_pred /*DEV*/, int32_t* path /*DEV*/, int32_t* n_acc /*DEV*/, int32_t* emitted /*DEV*/,
+                   int32_t* kv_len /*DEV*/);
+
 /* One pass of the loop for a host that sits in it (Sec. 3: predict, edit, verify, accept), with HOST
  * buffers: runs the draft modules; copies `cand` in (HOST int32 [batch, D+1], pinned memory makes
  * the copy asynchronous; an entry >= 0 replaces the draft modules' candidate at that slot, an entry

@@ -116,6 +116,10 @@ def load_library():
     lib.fm_step_host.argtypes = [vp, vp, vp, vp, vp]
     lib.fm_accept.restype = C.c_int
     lib.fm_accept.argtypes = [vp, vp, vp, vp, vp, vp]
+    lib.fm_verify_tree.restype = C.c_int
+    lib.fm_verify_tree.argtypes = [vp, vp, vp, i32, vp, f32p, f32p]
+    lib.fm_accept_tree.restype = C.c_int
+    lib.fm_accept_tree.argtypes = [vp, vp, vp, vp, vp, vp]
     lib.fm_generate.restype = C.c_int
     lib.fm_generate.argtypes = [vp, i32, vp, i32, vp, C.POINTER(FmTeacher), i32, C.c_int64, C.POINTER(FmStats)]
     lib.fm_verify_bytes.restype = C.c_double
@@ -207,6 +211,14 @@ def fm_step_host(ctx, cand_host_ptr, n_acc_host_ptr, emitted_host_ptr=None, kv_l
 
 def fm_accept(ctx, force_len_ptr=None, force_tok_ptr=None, n_acc_ptr=None, emitted_ptr=None, kv_len_ptr=None):
     return load_library().fm_accept(ctx, force_len_ptr, force_tok_ptr, n_acc_ptr, emitted_ptr, kv_len_ptr)
+
+
+def fm_verify_tree(ctx, tokens_ptr, parent_ptr, nodes, predicted_ptr=None, logits_ptr=None, margin_ptr=None):
+    return load_library().fm_verify_tree(ctx, tokens_ptr, parent_ptr, int(nodes), predicted_ptr, logits_ptr, margin_ptr)
+
+
+def fm_accept_tree(ctx, force_pred_ptr=None, path_ptr=None, n_acc_ptr=None, emitted_ptr=None, kv_len_ptr=None):
+    return load_library().fm_accept_tree(ctx, force_pred_ptr, path_ptr, n_acc_ptr, emitted_ptr, kv_len_ptr)
 
 
 def fm_generate(ctx, max_faces, out_tok_ptr, out_stride, out_len_ptr, teacher=None, plain=0, max_steps=0, stats=None):
@@ -436,6 +448,16 @@ class FlashMesh:
         self._after(cand, dl, dm)
         return cand, dl, dm
 
+    def draft_alternatives(self, top):
+        """Draft, and the `top` likeliest coordinate bins of every drafted position with their log probabilities among the bins: what
+        trees for `verify_tree` are made of.  Returns (cand [B, D+1], ids [B, D, top], logprobs [B, D, top], entropies [B, D]);
+        ids[:, :, 0] are the drafts wherever a bin was drafted.  (Rows of finished sequences mean nothing.)"""
+        from .trees import logprobs
+        B, D, n = self.batch, self.D, int(self.cfg.n_bins)
+        cand, dl, _ = self.draft(want_logits=True)
+        _, entropy, _, ids, lp = logprobs(dl.view(B * D, self.V)[:, :n], top=top)
+        return cand, ids.view(B, D, top), lp.view(B, D, top), entropy.view(B, D)
+
     def correct(self, cand, labels=None, use_history=False):
         """Edit the drafts of `cand` (int32 [B, D+1], device) in place with the per-point labels
         (int32 [B, D+1], device; None = the label head's of the last draft); returns `cand`."""
@@ -485,6 +507,38 @@ class FlashMesh:
                               kv.data_ptr()), "fm_accept")
         self._after(fl, ft, n_acc, em, kv)
         return n_acc, em, kv
+
+    def verify_tree(self, tokens, parent, want_logits=False):
+        """Verify trees of candidates: tokens, parent [B, nodes] int32 (node 0 the pending main token, parent -1).  Returns
+        (predicted [B, nodes], logits [B, nodes, V] or None, margins [B, nodes])."""
+        t = self.torch
+        tokens, parent = self._dev(tokens, t.int32), self._dev(parent, t.int32)
+        if tokens.dim() != 2 or tokens.shape != parent.shape or tokens.shape[0] != self.batch:
+            raise FmError(-1, "verify_tree: tokens and parent [batch, nodes]")
+        N = tokens.shape[1]
+        pred, mg = self._empty((self.batch, N), t.int32), self._empty((self.batch, N), t.float32)
+        lg = self._empty((self.batch, N, self.V), t.float32) if want_logits else None
+        self._before()
+        self._check(fm_verify_tree(self.ctx, tokens.data_ptr(), parent.data_ptr(), N, pred.data_ptr(), lg.data_ptr() if lg is not None else None,
+                                   mg.data_ptr()), "fm_verify_tree")
+        self._after(tokens, parent, pred, lg, mg)
+        self._tree_nodes = N
+        return pred, lg, mg
+
+    def accept_tree(self, force_pred=None):
+        """Accept the longest confirmed path of the last verify_tree: (path [B, nodes], n_acc [B], emitted [B, nodes], kv_len [B, 3])."""
+        t = self.torch
+        N = getattr(self, "_tree_nodes", 1)
+        fp = self._dev(force_pred, t.int32) if force_pred is not None else None
+        if fp is not None and fp.shape != (self.batch, N):
+            raise FmError(-1, "accept_tree: force_pred [batch, nodes]")
+        path, em = self._empty((self.batch, N), t.int32), self._empty((self.batch, N), t.int32)
+        n_acc, kv = self._empty((self.batch,), t.int32), self._empty((self.batch, 3), t.int32)
+        self._before()
+        self._check(fm_accept_tree(self.ctx, fp.data_ptr() if fp is not None else None, path.data_ptr(), n_acc.data_ptr(), em.data_ptr(),
+                                   kv.data_ptr()), "fm_accept_tree")
+        self._after(fp, path, n_acc, em, kv)
+        return path, n_acc, em, kv
 
     def step_host(self, cand_h, n_acc_h, emitted_h=None, kv_len_h=None):
         """One pass through fm_step_host; the arguments are host tensors (pinned for asynchronous

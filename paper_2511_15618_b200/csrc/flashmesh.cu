@@ -22,6 +22,7 @@
 #include "fm_gemm_tc.cuh"
 #include "fm_gemm_rows.cuh"
 #include "fm_kernels.cuh"
+#include "fm_hourglass_tree.cuh"
 #include "fm_prefill.cuh"
 
 namespace {
@@ -113,6 +114,8 @@ struct fm_ctx {
   } pre;
   std::vector<char> plan_host;
   int* limits_dev;
+  ht::Tree tree;                         // buffers of fm_verify_tree
+  char* tree_scratch;                    // its attention's workspace
   // generate
   GenOut* gen_dev;
   long long* stats_dev;
@@ -154,7 +157,7 @@ struct fm_ctx {
   bool gen_fresh;       // no fm_generate call since the last fm_prefill
   bool advanced;        // ... and no fm_accept
   std::vector<int> plen_host;
-  int phase;            // 0 created, 1 prefilled / accepted, 2 verified
+  int phase;            // 0 created, 1 prefilled / accepted, 2 verified, 3 a tree verified
   int64_t launches;
 };
 
@@ -380,6 +383,21 @@ void carve(fm_ctx* c, Carver& cv) {
   }
   c->gen_dev = cv.take<GenOut>(1);
   c->stats_dev = cv.take<long long>(FM_MAX_DRAFT + 4);
+  {
+    auto& t = c->tree;
+    const size_t R = align_up(B * dm.R1, 16), kvw = (size_t)dm.Hkv * dm.dh;
+    t.rows_alloc = (int)R;
+    for (int l = 0; l < 3; ++l) {
+      t.row[l] = cv.take<PackedRow>(R); t.par[l] = cv.take<int>(R); t.node[l] = cv.take<int>(R); t.len[l] = cv.take<int>(B);
+      t.z[l] = cv.take<float>(R * d);
+    }
+    for (int l = 0; l < 2; ++l) { t.low[l] = cv.take<int>(3 * R); t.up[l] = cv.take<int>(R); t.h[l] = cv.take<float>(R * d); t.tri[l] = cv.take<float>(R * 3 * d); }
+    t.off = cv.take<int>(B + 1); t.ident = cv.take<int>(B);
+    t.tok = cv.take<int>(R); t.pred = cv.take<int>(R); t.acc = cv.take<int>(R);
+    t.k = cv.take<bf16>(n_layers * R * kvw); t.v = cv.take<bf16>(n_layers * R * kvw);
+    const size_t few = tr::workspace_bytes(1, 1, dm.dh), most = tr::workspace_bytes(dm.R1, dm.H / dm.Hkv, dm.dh);
+    c->tree_scratch = cv.take<char>(few > most ? few : most);
+  }
   cv.off = align_up(cv.off, 256);
 }
 
@@ -1430,6 +1448,101 @@ int prefill_run(fm_ctx* c, const float* cond, const int* prompt, const int* off)
   return FM_OK;
 }
 
+// ------------------------------------------------------------------------------------------
+// a tree of candidates (see fm_hourglass_tree.cuh): the stages of a verify pass on the nodes' rows, in the prefill's buffers
+// ------------------------------------------------------------------------------------------
+int tree_attention(fm_ctx* c, int level, const LayerDev& L, const bf16* k_new, const bf16* v_new) {
+  const Dims& dm = c->dm;
+  const auto& t = c->tree;
+  const int slots = dm.P + dm.cap[level], ratio = fm_ratio(level);
+  tr::Args a{};
+  a.q = c->pre.q; a.k_new = k_new; a.v_new = v_new; a.out = c->pre.attn;
+  a.q_row = dm.H * dm.dh; a.new_row = dm.Hkv * dm.dh; a.out_row = 2 * dm.H * dm.dh; a.lo_off = dm.H * dm.dh;
+  a.k = reinterpret_cast<const char*>(L.K); a.v = reinterpret_cast<const char*>(L.V);
+  a.page = (int64_t)dm.Hkv * slots * dm.dh; a.head = (int64_t)slots * dm.dh; a.slot = dm.dh;
+  a.table = t.ident; a.lens = t.len[level]; a.row_off = t.off; a.parent = t.par[level]; a.status = c->st.status;
+  a.desc = reinterpret_cast<int4*>(c->tree_scratch);
+  a.part = reinterpret_cast<float*>(c->tree_scratch + tr::DESC_BYTES);
+  a.page_div = tr::div_by(slots);
+  a.n_pages = dm.max_batch; a.max_pages = 1; a.max_seqs = dm.max_batch; a.batch = c->batch; a.H = dm.H; a.Hkv = dm.Hkv; a.G = dm.H / dm.Hkv;
+  a.max_nodes = t.N; a.max_len = dm.P + (dm.max_tokens + ratio - 1) / ratio; a.window = dm.window[level]; a.n_prefix = dm.P;
+  // a level whose cache is shorter than a run is a ring
+  a.ring = dm.cap[level] < (dm.max_tokens + ratio - 1) / ratio ? dm.cap[level] : 0;
+  a.scale_log2 = 1.f;                                        // (in the queries already)
+  fm_cache fc{};
+  fc.k = L.K; fc.v = L.V; fc.page_stride = a.page; fc.head_stride = a.head; fc.slot_stride = a.slot;
+  fc.n_layers = 1; fc.n_pages = dm.max_batch; fc.page_slots = slots; fc.n_kv_heads = dm.Hkv; fc.head_dim = dm.dh; fc.dtype = FM_BF16;
+  a.tma = tr::make_maps(fc, 0, 1, a) ? 1 : 0;
+  c->launches += 2;
+  return tr::launch(a, FM_BF16, dm.dh, c->stream);
+}
+
+void tree_stack(fm_ctx* c, int R, int s, int first_layer, const float* next_gain, bool want_a, float* z) {
+  const Dims& dm = c->dm;
+  auto& pr = c->pre;
+  auto& t = c->tree;
+  const int level = STACK_LEVEL[s], d = dm.d, hd = dm.H * dm.dh, kvw = dm.Hkv * dm.dh, qkvw = hd + 2 * kvw;
+  const int nl = (int)c->layers[s].size(), ld = pr.rows[0];
+  float* x = pr.x[level];
+  for (int l = 0; l < nl && c->launch_error == FM_OK; ++l) {
+    const LayerDev& L = c->layers[s][l];
+    const bool last = l == nl - 1;
+    bf16 *kn = t.k + (size_t)(first_layer + l) * t.rows_alloc * kvw, *vn = t.v + (size_t)(first_layer + l) * t.rows_alloc * kvw;
+    // (the split nodes that the draft heads read: the input of the stack's last layer)
+    if (last && z != nullptr && cudaMemcpyAsync(z, x, (size_t)R * d * sizeof(float), cudaMemcpyDeviceToDevice, c->stream) != cudaSuccess) c->launch_error = FM_ERR_CUDA;
+    pf::Epi eq{};
+    eq.ssq_in = pr.ssq; eq.ssq_n = c->ssq_n; eq.ld_ssq = c->ssq_ld; eq.inv_d = 1.f / d; eq.eps = dm.eps;
+    eq.dm = dm; eq.rows = t.row[level]; eq.level = level; eq.rope = c->rope_tab; eq.qscale = (float)(1.4426950408889634 / sqrt((double)dm.dh));
+    eq.q = pr.q; eq.kbuf = kn; eq.vbuf = vn;
+    pf_gemm(c, pf::PF_QKV, L.Wqkv, pr.a, ld, qkvw, d, R, eq);
+    if (c->launch_error == FM_OK) c->launch_error = tree_attention(c, level, L, kn, vn);
+    tc::Epi eo{};
+    eo.x = x; eo.ldx = d; eo.add = 1; eo.gain = L.g2; eo.a_out = pr.a; eo.lda = 2 * d; eo.lo_off = d; eo.ssq_out = pr.ssq; eo.ld_ssq_out = c->ssq_ld;
+    gemm(c, L.Wo, pad128(d), 0, pr.attn, ld, 0, d, hd, R, nullptr, tc::EPI_RESID, eo, 2);
+    tc::Epi e1 = epi_plain(pr.wide, 2 * dm.dff);
+    e1.lo_off = dm.dff;
+    e1.ssq_in = pr.ssq; e1.ssq_n = c->ssq_n; e1.ld_ssq = c->ssq_ld; e1.inv_d_in = 1.f / d; e1.eps = dm.eps;
+    gemm(c, L.W1, pad128(dm.dff), 0, pr.a, ld, 0, dm.dff, d, R, nullptr, tc::EPI_GELU, e1, 2);
+    eo.gain = last ? next_gain : c->layers[s][l + 1].g1;
+    if (last && !want_a) { eo.a_out = nullptr; eo.ssq_out = nullptr; }
+    gemm(c, L.W2, pad128(d), 0, pr.wide, ld, 0, d, dm.dff, R, nullptr, tc::EPI_RESID, eo, 2);
+  }
+}
+
+void forward_tree(fm_ctx* c, const int* tokens, const int* parent, int nodes, int* pred_out, float* logits_out, float* margin_out) {
+  const Dims& dm = c->dm;
+  auto& pr = c->pre;
+  auto& t = c->tree;
+  const int B = c->batch, R = B * nodes, d = dm.d, th = row_threads(d);
+  t.N = nodes;
+  int first[5], n = 0;
+  for (int s = 0; s < 5; ++s) { first[s] = n; n += (int)c->layers[s].size(); }
+  LAUNCH(c, ht::map_kernel, (B + 32) / 32, 32, 0, dm, c->st, t, parent, B);
+  LAUNCH(c, ht::embed_kernel, R, th, 0, dm, c->st, t, tokens, (const bf16*)c->E, pr.x[0], (const float*)c->layers[0][0].g1, pr.a, pr.ssq, c->ssq_ld);
+  c->ssq_n = 1;
+  for (int up = 1; up <= 2; ++up) {                          // down
+    tree_stack(c, R, up - 1, first[up - 1], nullptr, false, nullptr);
+    LAUNCH(c, ht::gather_kernel, dim3(R, 3), th, 0, dm, t, up, (const float*)pr.x[up - 1], (const float*)(up == 1 ? c->hc_ring : c->hv_ring), pr.wide);
+    tc::Epi es{};
+    es.x = pr.x[up]; es.ldx = d; es.add = 0; es.gain = c->layers[up][0].g1; es.a_out = pr.a; es.lda = 2 * d; es.lo_off = d;
+    es.ssq_out = pr.ssq; es.ld_ssq_out = c->ssq_ld;
+    gemm(c, up == 1 ? c->S_cv : c->S_vf, pad128(d), 0, pr.wide, pr.rows[1], 0, d, 3 * d, R, nullptr, tc::EPI_RESID, es, 2);
+  }
+  tree_stack(c, R, 2, first[2], nullptr, true, t.z[2]);
+  for (int low = 1; low >= 0; --low) {                       // up
+    gemm(c, low == 1 ? c->U_fv : c->U_vc, pad128(3 * d), 0, pr.a, pr.rows[0], 0, 3 * d, d, R, nullptr, tc::EPI_F32, epi_plain(t.tri[low], 3 * d), 2);
+    LAUNCH(c, ht::upsample_kernel, R, th, 0, dm, t, low, (const float*)(low == 1 ? c->trif_ring : c->triv_ring), pr.x[low],
+           (const float*)c->layers[low == 1 ? 3 : 4][0].g1, pr.a, pr.ssq, c->ssq_ld);
+    c->ssq_n = 1;
+    const int s = low == 1 ? 3 : 4;
+    tree_stack(c, R, s, first[s], low == 0 ? c->g_out : nullptr, true, t.z[low]);
+  }
+  tc::Epi el = epi_plain(c->logits, dm.Vpad);
+  el.ssq_in = pr.ssq; el.ssq_n = c->ssq_n; el.ld_ssq = c->ssq_ld; el.inv_d_in = 1.f / d; el.eps = dm.eps;
+  gemm(c, c->W_out, dm.Vpad, 0, pr.a, pr.rows[0], 0, dm.V, d, R, nullptr, tc::EPI_F32, el, 2);
+  LAUNCH(c, ht::top_kernel, R, 256, 0, dm, t, (const float*)c->logits, logits_out, pred_out, margin_out);
+}
+
 // what ends a pass of fm_generate
 void step_end(fm_ctx* c) {
   const Dims& dm = c->dm;
@@ -2019,6 +2132,31 @@ int fm_accept(fm_ctx* c, const int32_t* force_len, const int32_t* force_tok, int
   if (c->phase != 2) return FM_ERR_BAD_STATE;
   launch_pdl(c, dim3(1, 1, 1), accept_kernel, 1, accept_threads(c->batch), 0, c->dm, c->st, c->batch, force_len, force_tok, n_acc, emitted, kv_len,
              (const GenOut*)nullptr, 0);
+  CUDA_OK(cudaGetLastError());
+  if (c->launch_error != FM_OK) return c->launch_error;
+  c->advanced = true;
+  c->phase = 1;
+  return FM_OK;
+}
+
+int fm_verify_tree(fm_ctx* c, const int32_t* tokens, const int32_t* parent, int32_t nodes, int32_t* predicted, float* logits, float* margin) {
+  if (c == nullptr || tokens == nullptr || parent == nullptr || nodes < 1) return FM_ERR_INVALID_ARG;
+  if (c->phase < 1) return FM_ERR_BAD_STATE;
+  if (nodes > c->dm.R1 || c->batch * nodes > c->pre.rows[2] || c->batch > FM_MAX_TREES) return FM_ERR_CAPACITY;
+  forward_tree(c, tokens, parent, nodes, predicted, logits, margin);
+  CUDA_OK(cudaGetLastError());
+  if (c->launch_error != FM_OK) return c->launch_error;
+  c->phase = 3;
+  return FM_OK;
+}
+
+int fm_accept_tree(fm_ctx* c, const int32_t* force_pred, int32_t* path, int32_t* n_acc, int32_t* emitted, int32_t* kv_len) {
+  if (c == nullptr) return FM_ERR_INVALID_ARG;
+  if (c->phase != 3) return FM_ERR_BAD_STATE;
+  const int n_layers = c->pre.n_layers;
+  LAUNCH(c, ht::accept_kernel, 1, accept_threads(c->batch), 0, c->dm, c->st, c->tree, c->batch, force_pred, path, n_acc, emitted, kv_len);
+  LAUNCH(c, ht::commit_kernel<pf::LayerPtr>, dim3(c->batch * c->tree.N, n_layers + 3), 128, 0, c->dm, c->tree, (const pf::LayerPtr*)c->pre.layers, n_layers,
+         c->hc_ring, c->hv_ring, c->trif_ring, c->triv_ring, c->zc, c->zv, c->zf);
   CUDA_OK(cudaGetLastError());
   if (c->launch_error != FM_OK) return c->launch_error;
   c->advanced = true;

@@ -84,18 +84,6 @@ pg::Geo geo_of(const fm_cache& c) {
   return g;
 }
 
-tr::Div div_by(int d) {
-  tr::Div v{0, 0, d};
-  if (d > 1) {
-    int l = 0;
-    while ((1ll << l) < d) ++l;
-    const int p = 31 + l;                      // n * (2^p / d rounded up) >> p is exact for n < 2^31
-    v.mul = (uint32_t)(((1ull << p) + d - 1) / d);
-    v.shift = p - 32;
-  }
-  return v;
-}
-
 int check_tree(const fm_cache* c, const fm_tree_args* t) {
   const int rc = check_cache(c);
   if (rc != FM_OK) return rc;
@@ -113,9 +101,37 @@ int check_tree(const fm_cache* c, const fm_tree_args* t) {
   return FM_OK;
 }
 
+template <typename T, int R>
+int score_short(const lp::Args& a, cudaStream_t stream) {
+  lp::short_kernel<T, R><<<(a.rows + lp::SHORT_WARPS - 1) / lp::SHORT_WARPS, 32 * lp::SHORT_WARPS, 0, stream>>>(a);
+  return launched();
+}
+
+// Rows whose vectors fit into a warp's registers (64 values a lane) take a warp, longer ones a block: of 256 threads, or of 512
+// where there are too few rows to fill the SMs with the smaller one.
+template <typename T>
+int score_rows(const lp::Args& a, cudaStream_t stream) {
+  constexpr int N = lp::Vec<T>::N, MOST = 64 / N;
+  const int vectors = (a.vocab / N + 31) / 32;               // a lane
+  if (vectors <= MOST) {
+    if (vectors <= 1) return score_short<T, 1>(a, stream);
+    if (vectors <= MOST / 4) return score_short<T, MOST / 4>(a, stream);
+    if (vectors <= MOST / 2) return score_short<T, MOST / 2>(a, stream);
+    return score_short<T, MOST>(a, stream);
+  }
+  if (a.rows >= 2 * 148) {
+    lp::long_kernel<T, 256, 8><<<a.rows, 256, 8 * 256 * 16, stream>>>(a);
+  } else {
+    static std::atomic<uint64_t> asked{0};
+    if (!allow_smem(lp::long_kernel<T, 512, 8>, 8 * 512 * 16, asked)) return FM_ERR_CUDA;
+    lp::long_kernel<T, 512, 8><<<a.rows, 512, 8 * 512 * 16, stream>>>(a);
+  }
+  return launched();
+}
+
 // Rows that share keys (nodes x heads of a group): up to 16 take the warp-level form, more the tensor cores' tiles of 128.
 inline bool few_rows(int max_nodes, int group) { return (int64_t)max_nodes * group <= 16; }
-constexpr size_t DESC_BYTES = 8192;                          // of up to 2 * 148 CTAs
+using tr::DESC_BYTES;
 static_assert(DESC_BYTES >= 2 * tr::SMS * sizeof(int4), "");
 static_assert(tr::Rows16<128>::C == tr::Rows128<64>::C && tr::Rows16<128>::C == tr::Rows128<128>::C, "make_maps: one chunk for the three of them");
 static_assert(tr::Rows16<128>::FIXED + tr::plan_bytes(FM_MAX_TREES) <= 227 * 1024 && tr::Rows128<128>::FIXED + tr::plan_bytes(FM_MAX_TREES) <= 227 * 1024, "");
@@ -137,9 +153,10 @@ EncodeTiledFn encode_tiled_fn() {
 // A layer's pool as (features, slots, heads, pages), boxes of 64 features and min(page, chunk) slots, 128-byte swizzle.
 // Boxes have to fill a chunk evenly and start where the swizzle does (8 rows); other page sizes, and strides that a map
 // cannot hold, are copied by threads.
-bool make_maps(const fm_cache& c, int layer, int chunk, tr::Args& a) {
+// (One page a sequence: any size from a chunk up, what lies behind the last slot reads as zeros.)
+bool make_maps_of(const fm_cache& c, int layer, int max_pages, int chunk, tr::Args& a) {
   const int ps = c.page_slots;
-  if (ps % 8 != 0 || (chunk % ps != 0 && ps % chunk != 0)) return false;
+  if (!(max_pages == 1 && ps >= chunk) && (ps % 8 != 0 || (chunk % ps != 0 && ps % chunk != 0))) return false;
   const EncodeTiledFn fn = encode_tiled_fn();
   if (fn == nullptr) return false;
   const int64_t most = (int64_t)1 << 39;
@@ -185,35 +202,31 @@ int tree_attention(const tr::Args& a, cudaStream_t stream) {
   return e == cudaSuccess ? FM_OK : FM_ERR_CUDA;
 }
 
-template <typename T, int R>
-int score_short(const lp::Args& a, cudaStream_t stream) {
-  lp::short_kernel<T, R><<<(a.rows + lp::SHORT_WARPS - 1) / lp::SHORT_WARPS, 32 * lp::SHORT_WARPS, 0, stream>>>(a);
-  return launched();
-}
-
-// Rows whose vectors fit into a warp's registers (64 values a lane) take a warp, longer ones a block: of 256 threads, or of 512
-// where there are too few rows to fill the SMs with the smaller one.
-template <typename T>
-int score_rows(const lp::Args& a, cudaStream_t stream) {
-  constexpr int N = lp::Vec<T>::N, MOST = 64 / N;
-  const int vectors = (a.vocab / N + 31) / 32;               // a lane
-  if (vectors <= MOST) {
-    if (vectors <= 1) return score_short<T, 1>(a, stream);
-    if (vectors <= MOST / 4) return score_short<T, MOST / 4>(a, stream);
-    if (vectors <= MOST / 2) return score_short<T, MOST / 2>(a, stream);
-    return score_short<T, MOST>(a, stream);
-  }
-  if (a.rows >= 2 * 148) {
-    lp::long_kernel<T, 256, 8><<<a.rows, 256, 8 * 256 * 16, stream>>>(a);
-  } else {
-    static std::atomic<uint64_t> asked{0};
-    if (!allow_smem(lp::long_kernel<T, 512, 8>, 8 * 512 * 16, asked)) return FM_ERR_CUDA;
-    lp::long_kernel<T, 512, 8><<<a.rows, 512, 8 * 512 * 16, stream>>>(a);
-  }
-  return launched();
-}
-
 }  // namespace
+
+namespace tr {
+
+Div div_by(int d) {
+  Div v{0, 0, d};
+  if (d > 1) {
+    int l = 0;
+    while ((1ll << l) < d) ++l;
+    const int p = 31 + l;                      // n * (2^p / d rounded up) >> p is exact for n < 2^31
+    v.mul = (uint32_t)(((1ull << p) + d - 1) / d);
+    v.shift = p - 32;
+  }
+  return v;
+}
+size_t workspace_bytes(int max_nodes, int group, int head_dim) { return tree_bytes(few_rows(max_nodes, group), head_dim); }
+bool make_maps(const fm_cache& c, int layer, int max_pages, Args& a) {
+  return make_maps_of(c, layer, max_pages, few_rows(a.max_nodes, a.G) && c.head_dim == 64 ? Rows16<64>::C : Rows16<128>::C, a);
+}
+int launch(const Args& a, int dtype, int head_dim, cudaStream_t stream) {
+  if (dtype == FM_BF16) return head_dim == 64 ? tree_attention<bf16, 64>(a, stream) : tree_attention<bf16, 128>(a, stream);
+  return head_dim == 64 ? tree_attention<__half, 64>(a, stream) : tree_attention<__half, 128>(a, stream);
+}
+
+}  // namespace tr
 
 extern "C" {
 
@@ -286,7 +299,7 @@ int fm_pages_compact(const fm_pages* p, const fm_cache* c, int32_t* used, void* 
 
 size_t fm_tree_attention_bytes(const fm_cache* cache, const fm_tree_args* args) {
   if (check_tree(cache, args) != FM_OK) return 0;
-  return tree_bytes(few_rows(args->max_nodes, args->n_heads / cache->n_kv_heads), cache->head_dim);
+  return tr::workspace_bytes(args->max_nodes, args->n_heads / cache->n_kv_heads, cache->head_dim);
 }
 
 int fm_tree_attention(const fm_cache* c, int32_t layer, const fm_tree_args* t, void* workspace, size_t workspace_bytes, void* stream) {
@@ -303,17 +316,15 @@ int fm_tree_attention(const fm_cache* c, int32_t layer, const fm_tree_args* t, v
   a.table = t->table; a.lens = t->lens; a.seqs = t->seqs; a.row_off = t->row_off; a.parent = t->parent; a.status = t->status;
   a.desc = static_cast<int4*>(workspace);
   a.part = reinterpret_cast<float*>(static_cast<char*>(workspace) + DESC_BYTES);
-  a.page_div = div_by(c->page_slots);
+  a.page_div = tr::div_by(c->page_slots);
   a.n_pages = c->n_pages; a.max_pages = t->max_pages; a.max_seqs = t->max_seqs; a.batch = t->batch;
   a.H = t->n_heads; a.Hkv = c->n_kv_heads; a.G = t->n_heads / c->n_kv_heads; a.max_nodes = t->max_nodes;
   const int64_t holds = (int64_t)t->max_pages * c->page_slots;
   a.max_len = t->max_len < holds ? t->max_len : (int)holds;
   a.window = t->window; a.n_prefix = t->n_prefix;
   a.scale_log2 = t->scale * 1.4426950408889634f;
-  const bool few = few_rows(a.max_nodes, a.G);
-  a.tma = make_maps(*c, layer, few && c->head_dim == 64 ? tr::Rows16<64>::C : tr::Rows16<128>::C, a) ? 1 : 0;
-  if (c->dtype == FM_BF16) return c->head_dim == 64 ? tree_attention<bf16, 64>(a, as_stream(stream)) : tree_attention<bf16, 128>(a, as_stream(stream));
-  return c->head_dim == 64 ? tree_attention<__half, 64>(a, as_stream(stream)) : tree_attention<__half, 128>(a, as_stream(stream));
+  a.tma = tr::make_maps(*c, layer, t->max_pages, a) ? 1 : 0;
+  return tr::launch(a, c->dtype, c->head_dim, as_stream(stream));
 }
 
 int fm_tree_accept(const int32_t* tokens, const int32_t* parent, const int32_t* row_off, const int32_t* predicted, int32_t batch, int32_t* path,

@@ -43,6 +43,8 @@ struct Args {
   Div page_div;
   int n_pages, max_pages, max_seqs, batch, H, Hkv, G, max_nodes, max_len, window, n_prefix;
   float scale_log2;
+  int ring;                             // 0, or: positions behind the prefix wrap around after so many slots (one page per sequence)
+  int lo_off;                           // 0, or: rows are [hi | lo] bfloat16 terms, lo so many elements behind hi
   int tma;                              // the page size suits the boxes
   alignas(64) CUtensorMap map_k, map_v; // the layer's pool as [pages][heads][slots][head_dim], box 64 features x min(page, C) slots
 };
@@ -69,6 +71,12 @@ __device__ inline uint32_t finite_part(uint32_t v, bool& bad) {
   if ((v & E) == E) { v &= 0xffff0000u; bad = true; }
   if (((v >> 16) & E) == E) { v &= 0x0000ffffu; bad = true; }
   return v;
+}
+
+// a value that the rounding of a pair to T lost, as a pair of bfloat16 (rows of two terms)
+__device__ inline uint32_t pack_rest(float x, float y, uint32_t hi) {
+  const float2 h = unpack(hi, bf16());
+  return ptx::pack_bf16(__fsub_rn(x, h.x), __fsub_rn(y, h.y));
 }
 
 __device__ inline float ex2(float x) {
@@ -195,6 +203,16 @@ __device__ inline Chunk chunk_of(const Seq& s, int c) {
   return k;
 }
 
+// where position-slot `slot` of a sequence lies in its pages
+__device__ inline int place_of(const Args& a, int slot) { return a.ring > 0 && slot >= a.n_prefix ? a.n_prefix + (slot - a.n_prefix) % a.ring : slot; }
+// is the chunk brought as boxes?  (not where it runs over the end of a ring)
+__device__ inline bool boxed(const Args& a, const Chunk& k) {
+  if (!a.tma || k.tree) return false;
+  if (a.ring == 0) return true;
+  const int last = k.start + k.n - 1;
+  return last < a.n_prefix || place_of(a, last) - place_of(a, k.start) == k.n - 1;
+}
+
 // ---- prefix sums over the sequences, by a block of THREADS
 template <int C, int ROWS, int THREADS>
 __device__ inline void make_plan(const Args& a, Plan& p, int4* info, long long* base, int* tile_base, long long* sh) {
@@ -263,7 +281,7 @@ __device__ inline int parts_of(const Args& a, const Plan& p, int cta, long long 
 struct Box { int id, in_page; };                             // id -1: none
 template <int C>
 __device__ inline Box box_of(const Args& a, const Seq& s, const Chunk& k, int lane) {
-  const int rows = min(a.page_div.d, C), slot = k.start + lane * rows;         // (at most C / 8 = 16 boxes)
+  const int rows = min(a.page_div.d, C), slot = place_of(a, k.start + lane * rows);        // (at most C / 8 = 16 boxes)
   Box x{-1, 0};
   if (!k.tree && lane * rows < k.n) {
     const int pi = a.page_div(slot);
@@ -306,7 +324,7 @@ __device__ inline void request_pieces(const Args& a, const Seq& s, const Chunk& 
       kp = static_cast<const T*>(a.k_new); vp = static_cast<const T*>(a.v_new);
       if (there) at = (int64_t)(s.r0 + k.start + r) * a.new_row + hk * DH;
     } else if (there) {
-      const int slot = k.start + r, pi = a.page_div(slot), id = __ldg(table + pi);
+      const int slot = place_of(a, k.start + r), pi = a.page_div(slot), id = __ldg(table + pi);
       if (id < 0 || id >= a.n_pages) {
         there = false;
         if (a.status != nullptr) atomicMin(a.status, FM_ERR_INVALID_ARG);
@@ -477,7 +495,7 @@ __global__ void __launch_bounds__(Rows16<DH>::THREADS, 1) rows16_kernel(const __
         const int st = i % ST;
         if (i >= ST && !(ok = wait(empty + st, ((i / ST) - 1) & 1))) break;
         unsigned char* Ks = sm + st * CF::STAGE;
-        if (a.tma && !k.tree) {
+        if (boxed(a, k)) {
           if (written > 0) { --written; ptx::fence_proxy_async(); }
           request_boxes<C>(a, map, x0, k, x, first, step, hk, Ks + off, full + st, lane);
         } else {
@@ -718,7 +736,10 @@ __global__ void __launch_bounds__(Rows16<DH>::THREADS, 1) rows16_kernel(const __
         if (!live) { mm = -INFINITY; l = o0 = o1 = 0.f; }
         if (whole) {
           const float inv = live ? 1.f / l : 0.f;
-          *reinterpret_cast<uint32_t*>(static_cast<T*>(a.out) + (int64_t)(s.r0 + nd) * a.out_row + (hk * a.G + gh) * DH + col) = pack(o0 * inv, o1 * inv, T());
+          T* at = static_cast<T*>(a.out) + (int64_t)(s.r0 + nd) * a.out_row + (hk * a.G + gh) * DH + col;
+          const uint32_t hi = pack(o0 * inv, o1 * inv, T());
+          *reinterpret_cast<uint32_t*>(at) = hi;
+          if (a.lo_off > 0) *reinterpret_cast<uint32_t*>(at + a.lo_off) = pack_rest(o0 * inv, o1 * inv, hi);
           if (col == 0 && a.lse != nullptr) a.lse[(int64_t)(s.r0 + nd) * a.H + hk * a.G + gh] = live ? (mm + log2f(l)) * 0.6931471805599453f : -INFINITY;
         } else {
           float* row = part_at + (size_t)i * (DH + 2);
@@ -824,7 +845,7 @@ __device__ inline bool uneven_chunk(const Args& a, const Seq& s, const Chunk& k)
 template <typename T, int DH>
 __device__ inline const T* values_of(const Args& a, const Seq& s, const Chunk& k, int hk, int key) {
   if (k.tree) return static_cast<const T*>(a.v_new) + (int64_t)(s.r0 + k.start + key) * a.new_row + hk * DH;
-  const int at = k.start + key, pi = a.page_div(at), id = a.table[(int64_t)s.seq * a.max_pages + pi];
+  const int at = place_of(a, k.start + key), pi = a.page_div(at), id = a.table[(int64_t)s.seq * a.max_pages + pi];
   if (id < 0 || id >= a.n_pages) return nullptr;
   return reinterpret_cast<const T*>(a.v) + id * a.page + hk * a.head + (int64_t)(at - pi * a.page_div.d) * a.slot;
 }
@@ -890,7 +911,7 @@ __global__ void __launch_bounds__(Rows128<DH>::THREADS, 2) rows128_kernel(const 
         const int st = i % ST;
         unsigned char *Ks = ring + st * STAGE, *Vs = Ks + TILE;
         if (i >= ST && !(ok = wait(room + st, ((i / ST) - 1) & 1))) break;
-        if (a.tma && !k.tree) {
+        if (boxed(a, k)) {
           // (both halves of a box in a lane: they land on one barrier, which every lane arrives on once)
           const CUtensorMap* map = v ? &a.map_v : &a.map_k;
           const int rows = min(a.page_div.d, C);
@@ -1144,11 +1165,15 @@ __global__ void __launch_bounds__(Rows128<DH>::THREADS, 2) rows128_kernel(const 
         } else if (whole) {
 #pragma unroll
           for (int j = 0; j < 32; j += 8) {
-            uint32_t p[4];
+            uint32_t p[4], q[4];
 #pragma unroll
-            for (int k = 0; k < 4; ++k)                      // (a row out of use: zeros, whatever the product holds)
-              p[k] = live ? pack(__uint_as_float(o[j + 2 * k]) * inv, __uint_as_float(o[j + 2 * k + 1]) * inv, T()) : 0u;
+            for (int k = 0; k < 4; ++k) {                    // (a row out of use: zeros, whatever the product holds)
+              const float u = live ? __uint_as_float(o[j + 2 * k]) * inv : 0.f, v = live ? __uint_as_float(o[j + 2 * k + 1]) * inv : 0.f;
+              p[k] = pack(u, v, T());
+              q[k] = pack_rest(u, v, p[k]);
+            }
             *reinterpret_cast<uint4*>(op + j0 + j) = make_uint4(p[0], p[1], p[2], p[3]);
+            if (a.lo_off > 0) *reinterpret_cast<uint4*>(op + a.lo_off + j0 + j) = make_uint4(q[0], q[1], q[2], q[3]);
           }
         } else {
 #pragma unroll
@@ -1241,7 +1266,11 @@ __global__ void __launch_bounds__(256) merge_kernel(const __grid_constant__ Args
     const float inv = live ? 1.f / l : 0.f;
     T* out = static_cast<T*>(a.out) + (int64_t)(r0 + nd) * a.out_row + (int64_t)h * DH;
 #pragma unroll
-    for (int j = 0; j < CL; ++j) reinterpret_cast<unsigned short*>(out)[lane + 32 * j] = (unsigned short)pack(o[j] * inv, 0.f, T());
+    for (int j = 0; j < CL; ++j) {
+      const uint32_t hi = pack(o[j] * inv, 0.f, T());
+      reinterpret_cast<unsigned short*>(out)[lane + 32 * j] = (unsigned short)hi;
+      if (a.lo_off > 0) reinterpret_cast<unsigned short*>(out)[a.lo_off + lane + 32 * j] = (unsigned short)pack_rest(o[j] * inv, 0.f, hi);
+    }
     if (lane == 0 && a.lse != nullptr) a.lse[(int64_t)(r0 + nd) * a.H + h] = live ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
   }
 }
@@ -1249,38 +1278,53 @@ __global__ void __launch_bounds__(256) merge_kernel(const __grid_constant__ Args
 // ------------------------------------------------------------------------------------------
 // the longest confirmed path: a warp per tree, eight nodes a lane
 // ------------------------------------------------------------------------------------------
-__global__ void __launch_bounds__(128) accept_kernel(const int* tokens, const int* parent, const int* row_off, const int* predicted, int batch,
-                                                     int* path, int path_stride, int* n_acc, int* next_tok) {
+// By a warp: calls put(i, node) in lane 0 for the nodes of the path, returns their number; `next`: the prediction at the last one.
+template <typename Put>
+__device__ inline int walk_path(const int* tokens, const int* parent, const int* predicted, int n, int lane, int& next, Put put) {
   constexpr int PER = FM_MAX_TREE_NODES / 32;
-  const int b = blockIdx.x * 4 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
-  if (b >= batch) return;
-  const int r0 = row_off[b], n = r0 < 0 ? 0 : min(min(row_off[b + 1] - r0, FM_MAX_TREE_NODES), path_stride);
   int par[PER], tok[PER], pre[PER];
+  n = min(n, FM_MAX_TREE_NODES);
 #pragma unroll
   for (int k = 0; k < PER; ++k) {
     const int i = k * 32 + lane;
-    par[k] = i < n ? parent[r0 + i] : -2;
-    tok[k] = i < n ? tokens[r0 + i] : 0;
-    pre[k] = i < n ? predicted[r0 + i] : 0;
+    par[k] = i < n ? parent[i] : -2;
+    tok[k] = i < n ? tokens[i] : 0;
+    pre[k] = i < n ? predicted[i] : 0;
   }
-  int cur = n > 0 && __shfl_sync(0xffffffffu, par[0], 0) == -1 ? 0 : -1, at = 0, want = -1;
+  int cur = n > 0 && __shfl_sync(0xffffffffu, par[0], 0) == -1 ? 0 : -1, at = 0;
   while (cur >= 0) {                                         // (every step goes to a later node)
-    if (lane == 0) path[(int64_t)b * path_stride + at] = cur;
+    if (lane == 0) put(at, cur);
     ++at;
     int mine = 0;
 #pragma unroll
     for (int k = 0; k < PER; ++k) if ((cur >> 5) == k) mine = pre[k];
-    want = __shfl_sync(0xffffffffu, mine, cur & 31);
-    int next = -1;
+    next = __shfl_sync(0xffffffffu, mine, cur & 31);
+    int child = -1;
 #pragma unroll
     for (int k = 0; k < PER; ++k) {
-      const unsigned hit = __ballot_sync(0xffffffffu, par[k] == cur && tok[k] == want && k * 32 + lane > cur);
-      if (next < 0 && hit != 0) next = k * 32 + __ffs(hit) - 1;
+      const unsigned hit = __ballot_sync(0xffffffffu, par[k] == cur && tok[k] == next && k * 32 + lane > cur);
+      if (child < 0 && hit != 0) child = k * 32 + __ffs(hit) - 1;
     }
-    cur = next;
+    cur = child;
   }
-  for (int j = at + lane; j < path_stride; j += 32) path[(int64_t)b * path_stride + j] = -1;
-  if (lane == 0) { n_acc[b] = at; next_tok[b] = at > 0 ? want : -1; }
+  return at;
 }
+static __global__ void __launch_bounds__(128) accept_kernel(const int* tokens, const int* parent, const int* row_off, const int* predicted, int batch,
+                                                     int* path, int path_stride, int* n_acc, int* next_tok) {
+  const int b = blockIdx.x * 4 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+  if (b >= batch) return;
+  const int r0 = row_off[b], n = r0 < 0 ? 0 : min(row_off[b + 1] - r0, path_stride);
+  int next = -1;
+  const int at = walk_path(tokens + r0, parent + r0, predicted + r0, n, lane, next, [&](int i, int node) { path[(int64_t)b * path_stride + i] = node; });
+  for (int j = at + lane; j < path_stride; j += 32) path[(int64_t)b * path_stride + j] = -1;
+  if (lane == 0) { n_acc[b] = at; next_tok[b] = at > 0 ? next : -1; }
+}
+
+constexpr size_t DESC_BYTES = 8192;      // in front of a workspace's parts: what the merge has to do, of up to 2 * SMS CTAs
+// Launches, for the entry points and for the context's own passes (fm_ops.cu).
+size_t workspace_bytes(int max_nodes, int group, int head_dim);
+bool make_maps(const fm_cache& c, int layer, int max_pages, Args& a);          // a.max_nodes and a.G are set
+int launch(const Args& a, int dtype, int head_dim, cudaStream_t stream);
+Div div_by(int d);
 
 }  // namespace tr

@@ -148,7 +148,7 @@ def test_scores_refuse(lib):
 def test_division_of_slots_by_the_page_size():
     """The multiplication that the kernels divide with, from the source's formula: exact for every slot below 2^31."""
     text = open(os.path.join(os.path.dirname(T.__file__), "csrc", "fm_ops.cu")).read()
-    body = re.search(r"tr::Div div_by\(int d\) \{(.*?)\n\}", text, re.S).group(1)
+    body = re.search(r"Div div_by\(int d\) \{(.*?)\n\}", text, re.S).group(1)
     assert "const int p = 31 + l;" in body and "((1ull << p) + d - 1) / d" in body and "v.shift = p - 32" in body and "(1ll << l) < d" in body
     rng = np.random.default_rng(0)
     for d in list(range(2, 300)) + [1000, 4095, 4096, 4097, 65535, 2 ** 20 + 1, 2 ** 30 - 1, 2 ** 30]:
