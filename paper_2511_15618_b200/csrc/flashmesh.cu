@@ -1463,7 +1463,7 @@ int tree_attention(fm_ctx* c, int level, const LayerDev& L, const bf16* k_new, c
   a.table = t.ident; a.lens = t.len[level]; a.row_off = t.off; a.parent = t.par[level]; a.status = c->st.status;
   a.desc = reinterpret_cast<int4*>(c->tree_scratch);
   a.part = reinterpret_cast<float*>(c->tree_scratch + tr::DESC_BYTES);
-  a.page_div = tr::div_by(slots);
+  a.page_div = tr::div_by(slots); a.g_div = tr::div_by(dm.H / dm.Hkv);
   a.n_pages = dm.max_batch; a.max_pages = 1; a.max_seqs = dm.max_batch; a.batch = c->batch; a.H = dm.H; a.Hkv = dm.Hkv; a.G = dm.H / dm.Hkv;
   a.max_nodes = t.N; a.max_len = dm.P + (dm.max_tokens + ratio - 1) / ratio; a.window = dm.window[level]; a.n_prefix = dm.P;
   // a level whose cache is shorter than a run is a ring

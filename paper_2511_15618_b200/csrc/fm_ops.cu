@@ -316,7 +316,7 @@ int fm_tree_attention(const fm_cache* c, int32_t layer, const fm_tree_args* t, v
   a.table = t->table; a.lens = t->lens; a.seqs = t->seqs; a.row_off = t->row_off; a.parent = t->parent; a.status = t->status;
   a.desc = static_cast<int4*>(workspace);
   a.part = reinterpret_cast<float*>(static_cast<char*>(workspace) + DESC_BYTES);
-  a.page_div = tr::div_by(c->page_slots);
+  a.page_div = tr::div_by(c->page_slots); a.g_div = tr::div_by(t->n_heads / c->n_kv_heads);
   a.n_pages = c->n_pages; a.max_pages = t->max_pages; a.max_seqs = t->max_seqs; a.batch = t->batch;
   a.H = t->n_heads; a.Hkv = c->n_kv_heads; a.G = t->n_heads / c->n_kv_heads; a.max_nodes = t->max_nodes;
   const int64_t holds = (int64_t)t->max_pages * c->page_slots;

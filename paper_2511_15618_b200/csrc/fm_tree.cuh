@@ -40,7 +40,7 @@ struct Args {
   int* status;
   float* part;                          // [CTAs * 2][ROWS][DH + 2]
   int4* desc;                           // [CTAs]: sequence, kv-head, tile, parts of the tile that starts here and is cut
-  Div page_div;
+  Div page_div, g_div;                  // by the slots of a page, by the heads of a group
   int n_pages, max_pages, max_seqs, batch, H, Hkv, G, max_nodes, max_len, window, n_prefix;
   float scale_log2;
   int ring;                             // 0, or: positions behind the prefix wrap around after so many slots (one page per sequence)
@@ -72,6 +72,10 @@ __device__ inline uint32_t finite_part(uint32_t v, bool& bad) {
   if (((v >> 16) & E) == E) { v &= 0x0000ffffu; bad = true; }
   return v;
 }
+
+// the larger of the halves' magnitudes (their bits without the sign), half by half: those of what is not finite stay on top
+template <typename T>
+__device__ inline uint32_t largest(uint32_t m, uint32_t v) { return __vmaxu2(m, v & 0x7fff7fffu); }
 
 // a value that the rounding of a pair to T lost, as a pair of bfloat16 (rows of two terms)
 __device__ inline uint32_t pack_rest(float x, float y, uint32_t hi) {
@@ -118,7 +122,7 @@ __device__ inline Seq sequence(const Args& a, int4 v) {
 }
 
 // ---- the cut of all chunks into shares.  A tile counts OVER chunks more than it has: what starting and ending it takes.
-constexpr int OVER = 2;
+constexpr int OVER = 4;
 struct Plan {
   const long long* base;                // [batch + 1] units in front of a sequence's
   const int* tile_base;                 // [batch + 1] tiles in front of a sequence's
@@ -156,8 +160,9 @@ template <int C, int ROWS>
 struct Walk {
   long long at, end;                    // next unit, end of the share
   Seq s;
-  int b, tile, c, c_end;                // tile of the sequence; next chunk of it, end of the share's part
+  int b, hk, mt, c, c_end;              // sequence, kv-head and tile of it; next chunk of it, end of the share's part
   long long tile_start;
+  bool inside;                          // next() has been called in this sequence
   __device__ void init(const Args& a, const Plan& p, int cta) {
     if (p.whole) {
       const bool any = cta < p.tile_base[p.batch];
@@ -171,6 +176,7 @@ struct Walk {
       b = at < end ? find(p.base, p.batch, at) : 0;
       s = sequence<C, ROWS>(a, p.info[b]);
     }
+    inside = false;
   }
   // the next tile, or part of one
   __device__ bool next(const Args& a, const Plan& p) {
@@ -178,10 +184,20 @@ struct Walk {
     if (at >= p.base[b + 1]) {
       do ++b; while (p.base[b + 1] == p.base[b]);
       s = sequence<C, ROWS>(a, p.info[b]);
+      inside = false;
     }
     const int units = s.chunks + OVER;
-    tile = (int)((at - p.base[b]) / units);
-    tile_start = p.base[b] + (long long)tile * units;
+    if (inside) {
+      if (++mt == s.tiles) { mt = 0; ++hk; }
+      tile_start = at;
+    } else {
+      const long long in = at - p.base[b];
+      const int tile = (in >> 31) == 0 ? (int)in / units : (int)(in / units);
+      hk = tile / s.tiles;
+      mt = tile - hk * s.tiles;
+      tile_start = p.base[b] + (long long)tile * units;
+      inside = true;
+    }
     c = max(0, (int)(at - tile_start) - OVER);               // (cuts lie behind the first OVER units or in front of them)
     c_end = (int)(end - tile_start < units ? end - tile_start : units) - OVER;
     at = tile_start + OVER + c_end;
@@ -347,7 +363,7 @@ __device__ inline void request_queries(const Args& a, const Seq& s, int hk, int 
   for (int r = t / PIECES; r < ROWS; r += step) {
     const int idx = mt * ROWS + r;
     const bool there = idx < M;
-    const int node = there ? idx / a.G : 0, gh = there ? idx - node * a.G : 0;
+    const int node = there ? a.g_div(idx) : 0, gh = there ? idx - node * a.G : 0;
     cp16(qs + ptx::swz128(r, piece & 7), static_cast<const T*>(a.q) + (int64_t)(s.r0 + node) * a.q_row + (hk * a.G + gh) * DH + piece * 8, there);
   }
 }
@@ -367,6 +383,19 @@ struct Tree {
   short depth[FM_MAX_TREE_NODES];
   int max_depth;
 };
+// Which of the keys k0 .. k0 + 31 of a chunk a row sees, a bit each (k0 a multiple of 16, a tree's chunks start at multiples of
+// 32; of a k0 that is none of 32 the lower 16 bits count).  node: the row's, -1: none; low: the first cached position it sees.
+__device__ inline uint32_t seen(const Args& a, const Tree& t, const Chunk& ck, int node, int depth, int low, int k0) {
+  auto below = [](int n) { return n <= 0 ? 0u : (n >= 32 ? ~0u : (1u << n) - 1u); };
+  const int at = ck.start + k0;
+  if (node < 0 || k0 >= ck.n) return 0u;
+  if (!ck.tree) return (below(a.n_prefix - at) | ~below(low - at)) & below(ck.n - k0);
+  uint32_t bits = t.reach[node][at >> 5] >> (at & 31);
+  if (a.window > 0 && depth >= a.window)
+    for (uint32_t left = bits; left != 0u; left &= left - 1u)
+      if (depth - t.depth[at + __ffs(left) - 1] >= a.window) bits &= ~(left & (0u - left));
+  return bits;
+}
 template <int THREADS, typename Sync>
 __device__ inline void build_tree(Tree& t, const int* parent, int n, int tid, Sync sync) {
   constexpr int PER = FM_MAX_TREE_NODES / THREADS;
@@ -429,14 +458,16 @@ __device__ inline void build_tree(Tree& t, const int* parent, int n, int tid, Sy
 // sixteen query rows a tile, warp-level MMAs
 // ------------------------------------------------------------------------------------------
 // Eight warps multiply: four take the even chunks, four the odd ones, each a fixed slice of a chunk with its own running maximum,
-// sum and output (base 2); their states are merged at the end of a tile.  Four warps load, queries of the next tile included.
+// sum and output (base 2).  At the end of a tile one of the two groups hands its states over and goes on, the other merges
+// and writes: they take turns.  Four warps load, queries and parents of the next tile included.
 template <int DH>
 struct Rows16 {
   static constexpr int ROWS = 16, C = DH == 64 ? 128 : 64, NW = 4, KPW = C / NW, STAGES = 4;
   static constexpr int TILE = C * DH * 2, STAGE = 2 * TILE, RING = STAGES * STAGE, Q = 16 * DH * 2;
   static constexpr int STATES = NW * 16 * (DH + 2) * 4;
   static constexpr int THREADS = 2 * NW * 32 + 128;
-  static constexpr int FIXED = RING + 2 * Q + STATES + (int)sizeof(Tree) + 1024 + 512;
+  static constexpr int PARENTS = FM_MAX_TREE_NODES * 4;
+  static constexpr int FIXED = RING + 2 * Q + 2 * PARENTS + STATES + (int)sizeof(Tree) + 1024 + 512;
   static int bytes(int batch) { return FIXED + plan_bytes(batch); }
 };
 
@@ -447,7 +478,8 @@ __global__ void __launch_bounds__(Rows16<DH>::THREADS, 1) rows16_kernel(const __
   extern __shared__ unsigned char smem_raw[];
   unsigned char* sm = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   unsigned char* sq = sm + CF::RING;                         // [2] queries
-  float* pw = reinterpret_cast<float*>(sq + 2 * CF::Q);      // [NW][16][DH] outputs
+  int* s_parent = reinterpret_cast<int*>(sq + 2 * CF::Q);    // [2] parents of the tile's sequence
+  float* pw = reinterpret_cast<float*>(s_parent + 2 * FM_MAX_TREE_NODES);      // [NW][16][DH] outputs
   float* ml = pw + NW * 16 * DH;                             // [NW][16][2] maxima and sums
   int4* s_info = reinterpret_cast<int4*>(pw + NW * 16 * (DH + 2));
   long long* s_base = reinterpret_cast<long long*>(s_info + a.batch);
@@ -456,11 +488,11 @@ __global__ void __launch_bounds__(Rows16<DH>::THREADS, 1) rows16_kernel(const __
   uint64_t *empty = full + ST, *q_full = empty + ST, *q_free = q_full + 2;
   Tree& tree = *reinterpret_cast<Tree*>(q_free + 2);
   int* s_tile_base = reinterpret_cast<int*>(&tree + 1);
-  __shared__ int s_fail, s_stop;                             // (s_stop: the multiplying warps' own, read between two of their barriers)
+  __shared__ int s_fail;
   const int warp = (int)ptx::uniform(threadIdx.x >> 5), lane = threadIdx.x & 31, g = lane >> 2, t4 = lane & 3;
   ptx::grid_dep_launch();
   if (threadIdx.x == 0) {
-    s_fail = s_stop = 0;
+    s_fail = 0;
     for (int i = 0; i < ST; ++i) { ptx::mbar_init(full + i, 128); ptx::mbar_init(empty + i, NW); }
     for (int i = 0; i < 2; ++i) { ptx::mbar_init(q_full + i, 128); ptx::mbar_init(q_free + i, 2 * NW); }
     ptx::fence_mbar_init();
@@ -483,10 +515,12 @@ __global__ void __launch_bounds__(Rows16<DH>::THREADS, 1) rows16_kernel(const __
     long long cut_end = 0;
     bool ok = true;
     while (ok && w.next(a, plan)) {
-      const int hk = w.tile / w.s.tiles, mt = w.tile - hk * w.s.tiles;
+      const int hk = w.hk, mt = w.mt;
       if (w.starts() && !w.ends()) { cut = make_int4(w.b, hk, mt, 1); cut_end = w.tile_start + w.s.chunks + OVER; }
       if (part >= 2 && !(ok = wait(q_free + (part & 1), ((part >> 1) - 1) & 1))) break;
       request_queries<T, DH, 16>(a, w.s, hk, mt, sq + (part & 1) * CF::Q, tid, 128);
+      for (int j = tid; j < w.s.n; j += 128)
+        asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(ptx::smem_u32(s_parent + (part & 1) * FM_MAX_TREE_NODES + j)), "l"(a.parent + w.s.r0 + j) : "memory");
       cp_arrive(q_full + (part & 1));
       ++part;
       Chunk k = chunk_of<C>(w.s, w.c);
@@ -514,12 +548,13 @@ __global__ void __launch_bounds__(Rows16<DH>::THREADS, 1) rows16_kernel(const __
     auto sync = [] { asm volatile("bar.sync 1, 256;" ::: "memory"); };
     const int group = warp >> 2, wg = warp & 3;
     int tree_of = -1, it = 0, part = 0;
+    bool ok = true;                                          // (when a wait has given up the warps still meet at their barriers)
     while (w.next(a, plan)) {
       const Seq& s = w.s;
-      const int hk = w.tile / s.tiles, mt = w.tile - hk * s.tiles, M = s.n * a.G;
-      if (tree_of != w.b) { build_tree<256>(tree, a.parent + s.r0, s.n, threadIdx.x, sync); tree_of = w.b; }
+      const int hk = w.hk, mt = w.mt, M = s.n * a.G;
       const bool whole = w.starts() && w.ends();
-      bool ok = wait(q_full + (part & 1), (part >> 1) & 1);
+      ok = ok && wait(q_full + (part & 1), (part >> 1) & 1);
+      if (tree_of != w.b) { build_tree<256>(tree, s_parent + (part & 1) * FM_MAX_TREE_NODES, s.n, threadIdx.x, sync); tree_of = w.b; }
       uint32_t qa[KS][4];
       {
         const uint32_t q = ptx::smem_u32(sq + (part & 1) * CF::Q);
@@ -530,14 +565,13 @@ __global__ void __launch_bounds__(Rows16<DH>::THREADS, 1) rows16_kernel(const __
         }
         __syncwarp();
         if (lane == 0) ptx::mbar_arrive(q_free + (part & 1));
-        ++part;
       }
       // the rows' nodes (-1: behind the last), depths, first cached positions behind the prefix that they see
       int node[2], depth[2], low[2];
 #pragma unroll
       for (int hr = 0; hr < 2; ++hr) {
         const int idx = mt * 16 + g + hr * 8;
-        node[hr] = idx < M ? idx / a.G : -1;
+        node[hr] = idx < M ? a.g_div(idx) : -1;
         depth[hr] = node[hr] >= 0 ? tree.depth[node[hr]] : 0;
         low[hr] = a.window > 0 ? s.len + depth[hr] - a.window + 1 : 0;
       }
@@ -590,25 +624,31 @@ __global__ void __launch_bounds__(Rows16<DH>::THREADS, 1) rows16_kernel(const __
         if (!all_vis) {
           // keys of this thread: n-tile nt, element e -> nt * 8 + 2 * t4 + e of the warp's slice
 #pragma unroll
-          for (int nt = 0; nt < NT; ++nt)
+          for (int hr = 0; hr < 2; ++hr) {
+            const uint32_t bits = seen(a, tree, ck, node[hr], depth[hr], low[hr], wg * KPW) >> (2 * t4);
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              const int k = wg * KPW + nt * 8 + 2 * t4 + e, at = ck.start + k;
+            for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-              for (int hr = 0; hr < 2; ++hr) {
-                bool vis = k < ck.n && node[hr] >= 0;
-                if (vis && ck.tree) vis = ((tree.reach[node[hr]][at >> 5] >> (at & 31)) & 1u) && (a.window == 0 || depth[hr] - tree.depth[at] < a.window);
-                else if (vis && uneven) vis = at < a.n_prefix || at >= low[hr];
-                if (!vis) sc[nt][hr * 2 + e] = -INFINITY;
-              }
-            }
+              for (int e = 0; e < 2; ++e)
+                if (!((bits >> (nt * 8 + e)) & 1u)) sc[nt][hr * 2 + e] = -INFINITY;
+          }
           // (what lies behind the length is whatever the page holds)
+          uint32_t most = 0u;
 #pragma unroll
           for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
             for (int dp = 0; dp < DH / 16; ++dp)
 #pragma unroll
-              for (int j = 0; j < 4; ++j) vf[kb][dp][j] = finite_part<T>(vf[kb][dp][j], bad);
+              for (int j = 0; j < 4; ++j) most = largest<T>(most, vf[kb][dp][j]);
+          (void)finite_part<T>(most, bad);
+          if (bad) {
+#pragma unroll
+            for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+              for (int dp = 0; dp < DH / 16; ++dp)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) vf[kb][dp][j] = finite_part<T>(vf[kb][dp][j], bad);
+          }
         }
         float scale[2], base[2];
 #pragma unroll
@@ -677,13 +717,15 @@ __global__ void __launch_bounds__(Rows16<DH>::THREADS, 1) rows16_kernel(const __
         __syncwarp();
         if (lane == 0) ptx::mbar_arrive(empty + st);
       }
-      if (!ok) s_fail = s_stop = 1;
+      if (!ok) s_fail = 1;
 #pragma unroll
       for (int hr = 0; hr < 2; ++hr) {
         lrun[hr] += __shfl_xor_sync(0xffffffffu, lrun[hr], 1);
         lrun[hr] += __shfl_xor_sync(0xffffffffu, lrun[hr], 2);
       }
-      // ---- the states: the odd chunks' to the same warp of the even ones, then those in warp order
+      // ---- the states: one group's to the same warps of the other, then those in warp order.  The groups take turns, so the
+      // one that writes states is the one that read the last ones.  Barriers 2 and 3 (the states are there) take turns too: a
+      // group may be a tile ahead of the other, not two.
       float* mine = pw + wg * 16 * DH;
       auto put = [&] {
 #pragma unroll
@@ -696,32 +738,35 @@ __global__ void __launch_bounds__(Rows16<DH>::THREADS, 1) rows16_kernel(const __
           *reinterpret_cast<float2*>(ml + (wg * 16 + g + 8) * 2) = make_float2(mrun[1], lrun[1]);
         }
       };
-      if (group == 1) put();
-      sync();
-      if (*reinterpret_cast<volatile int*>(&s_stop)) break;  // (every warp has set its word in front of the barrier: all leave)
-      if (group == 0) {
-#pragma unroll
-        for (int hr = 0; hr < 2; ++hr) {
-          const float2 q = *reinterpret_cast<const float2*>(ml + (wg * 16 + g + 8 * hr) * 2);
-          // (no chunk on one side: maximum -inf and sum 0; a sum that is no number goes through)
-          const float mm = fmaxf(mrun[hr], q.x), f0 = mrun[hr] == -INFINITY ? 1.f : ex2(mrun[hr] - mm), f1 = q.x == -INFINITY ? 1.f : ex2(q.x - mm);
-          lrun[hr] = (f0 == 0.f ? 0.f : lrun[hr] * f0) + (f1 == 0.f ? 0.f : q.y * f1);
-          mrun[hr] = mm;
-#pragma unroll
-          for (int i = 0; i < DH / 8; ++i) {
-            const float2 v = *reinterpret_cast<const float2*>(mine + (g + 8 * hr) * DH + i * 8 + 2 * t4);
-            o[i][2 * hr] = (f0 == 0.f ? 0.f : o[i][2 * hr] * f0) + (f1 == 0.f ? 0.f : v.x * f1);
-            o[i][2 * hr + 1] = (f0 == 0.f ? 0.f : o[i][2 * hr + 1] * f0) + (f1 == 0.f ? 0.f : v.y * f1);
-          }
-        }
-        __syncwarp();
+      const int odd = part++ & 1;
+      if (group != odd) {
         put();
+        asm volatile("bar.arrive %0, 256;" ::"r"(2 + odd) : "memory");
+        continue;
       }
-      sync();
+      asm volatile("bar.sync %0, 256;" ::"r"(2 + odd) : "memory");
+#pragma unroll
+      for (int hr = 0; hr < 2; ++hr) {
+        const float2 q = *reinterpret_cast<const float2*>(ml + (wg * 16 + g + 8 * hr) * 2);
+        // (no chunk on one side: maximum -inf and sum 0; a sum that is no number goes through)
+        const float mm = fmaxf(mrun[hr], q.x), f0 = mrun[hr] == -INFINITY ? 1.f : ex2(mrun[hr] - mm), f1 = q.x == -INFINITY ? 1.f : ex2(q.x - mm);
+        lrun[hr] = (f0 == 0.f ? 0.f : lrun[hr] * f0) + (f1 == 0.f ? 0.f : q.y * f1);
+        mrun[hr] = mm;
+#pragma unroll
+        for (int i = 0; i < DH / 8; ++i) {
+          const float2 v = *reinterpret_cast<const float2*>(mine + (g + 8 * hr) * DH + i * 8 + 2 * t4);
+          o[i][2 * hr] = (f0 == 0.f ? 0.f : o[i][2 * hr] * f0) + (f1 == 0.f ? 0.f : v.x * f1);
+          o[i][2 * hr + 1] = (f0 == 0.f ? 0.f : o[i][2 * hr + 1] * f0) + (f1 == 0.f ? 0.f : v.y * f1);
+        }
+      }
+      __syncwarp();
+      put();
+      auto sync4 = [&] { asm volatile("bar.sync %0, 128;" ::"r"(4 + group) : "memory"); };
+      sync4();
       const int rows_here = min(16, M - mt * 16);
       float* part_at = a.part + (size_t)(blockIdx.x * 2 + (w.starts() ? 1 : 0)) * 16 * (DH + 2);
-      for (int e = threadIdx.x; e < rows_here * (DH / 2); e += 256) {
-        const int i = e / (DH / 2), col = 2 * (e - i * (DH / 2)), idx = mt * 16 + i, nd = idx / a.G, gh = idx - nd * a.G;
+      for (int e = threadIdx.x & 127; e < rows_here * (DH / 2); e += 128) {
+        const int i = e / (DH / 2), col = 2 * (e - i * (DH / 2)), idx = mt * 16 + i, nd = a.g_div(idx), gh = idx - nd * a.G;
         const bool live = tree.reach[nd][nd >> 5] != 0u;
         float2 stt[NW];
         float mm = -INFINITY, l = 0.f, o0 = 0.f, o1 = 0.f;
@@ -747,7 +792,7 @@ __global__ void __launch_bounds__(Rows16<DH>::THREADS, 1) rows16_kernel(const __
           if (col == 0) *reinterpret_cast<float2*>(row + DH) = make_float2(mm, l);
         }
       }
-      sync();                                                // the states have been read
+      sync4();                                               // the states have been read
     }
   }
   __syncthreads();
@@ -903,8 +948,8 @@ __global__ void __launch_bounds__(Rows128<DH>::THREADS, 2) rows128_kernel(const 
     long long cut_end = 0;
     bool ok = true;
     while (ok && w.next(a, plan)) {
-      const int hk = w.tile / w.s.tiles;
-      if (w.starts() && !w.ends()) { cut = make_int4(w.b, hk, w.tile - hk * w.s.tiles, 1); cut_end = w.tile_start + w.s.chunks + OVER; }
+      const int hk = w.hk;
+      if (w.starts() && !w.ends()) { cut = make_int4(w.b, hk, w.mt, 1); cut_end = w.tile_start + w.s.chunks + OVER; }
       Chunk k = chunk_of<C>(w.s, w.c);
       Box x = box_of<C>(a, w.s, k, lane);
       for (int c = w.c; c < w.c_end; ++c, ++i) {
@@ -947,10 +992,10 @@ __global__ void __launch_bounds__(Rows128<DH>::THREADS, 2) rows128_kernel(const 
     int i = 0, part = 0;
     bool ok = true;
     while (ok && w.next(a, plan)) {
-      const int hk = w.tile / w.s.tiles;
+      const int hk = w.hk;
       // the tile's queries, once the scores of the tile before have been multiplied
       if (part > 0 && !(ok = wait(q_free, (part - 1) & 1))) break;
-      request_queries<T, DH, 128>(a, w.s, hk, w.tile - hk * w.s.tiles, sm, lane, 32);
+      request_queries<T, DH, 128>(a, w.s, hk, w.mt, sm, lane, 32);
       asm volatile("cp.async.wait_all;" ::: "memory");
       ptx::fence_proxy_async();
       ptx::mbar_arrive(q_full);
@@ -1036,24 +1081,12 @@ __global__ void __launch_bounds__(Rows128<DH>::THREADS, 2) rows128_kernel(const 
     bool ok = true;
     while (w.next(a, plan)) {
       const Seq& s = w.s;
-      const int hk = w.tile / s.tiles, mt = w.tile - hk * s.tiles, idx = mt * 128 + i_row, M = s.n * a.G;
+      const int hk = w.hk, mt = w.mt, idx = mt * 128 + i_row, M = s.n * a.G;
       if (tree_of != w.b) { build_tree<256>(tree, a.parent + s.r0, s.n, tid, sync); tree_of = w.b; }
       const bool whole = w.starts() && w.ends();
       const bool there = idx < M;
-      const int node = there ? idx / a.G : 0, gh = there ? idx - node * a.G : 0, depth = there ? tree.depth[node] : 0;
+      const int node = there ? a.g_div(idx) : 0, gh = there ? idx - node * a.G : 0, depth = there ? tree.depth[node] : 0;
       const int low = a.window > 0 ? s.len + depth - a.window + 1 : 0, low_all = a.window > 0 ? s.len + tree.max_depth - a.window + 1 : 0;
-      auto visible = [&](const Chunk& ck, int k0) {          // keys k0 .. k0 + 31 of a chunk, a bit each (k0 and a tree's chunks start at multiples of 32)
-        auto below = [](int n) { return n <= 0 ? 0u : (n >= 32 ? ~0u : (1u << n) - 1u); };
-        const int at = ck.start + k0;
-        if (!there) return 0u;
-        if (!ck.tree) return (below(a.n_prefix - at) | ~below(low - at)) & below(ck.n - k0);
-        if (k0 >= ck.n) return 0u;
-        uint32_t bits = tree.reach[node][at >> 5];
-        if (a.window > 0 && depth >= a.window)
-          for (uint32_t left = bits; left != 0u; left &= left - 1u)
-            if (depth - tree.depth[at + __ffs(left) - 1] >= a.window) bits &= ~(left & (0u - left));
-        return bits;
-      };
       float m = -INFINITY, l = 0.f;                          // the maximum in use (times scale, base 2), this half's sum
       for (int c = w.c; c < w.c_end; ++c, ++it) {
         const Chunk ck = chunk_of<C>(s, c);
@@ -1069,7 +1102,7 @@ __global__ void __launch_bounds__(Rows128<DH>::THREADS, 2) rows128_kernel(const 
         __syncwarp();
         if (lane == 0) ptx::mbar_arrive(s_read);
         if (!all_vis) {
-          const uint32_t bits = visible(ck, HC * half);
+          const uint32_t bits = seen(a, tree, ck, there ? node : -1, depth, low, HC * half);
 #pragma unroll
           for (int j = 0; j < HC; ++j)
             if (!((bits >> j) & 1u)) r[j] = 0xff800000u;     // -inf: exponential 0
@@ -1149,7 +1182,7 @@ __global__ void __launch_bounds__(Rows128<DH>::THREADS, 2) rows128_kernel(const 
             const Chunk ck = chunk_of<C>(s, c);
             if (!uneven_chunk<C>(a, s, ck)) continue;
             for (int k = 0; k < ck.n; ++k) {
-              if (!((visible(ck, k & ~31) >> (k & 31)) & 1u)) continue;
+              if (!((seen(a, tree, ck, node, depth, low, k & ~31) >> (k & 31)) & 1u)) continue;
               const T* v = values_of<T, DH>(a, s, ck, hk, k);
               if (v == nullptr) continue;
 #pragma unroll
@@ -1261,7 +1294,7 @@ __global__ void __launch_bounds__(256) merge_kernel(const __grid_constant__ Args
       for (int j = 0; j < CL; ++j) o2[j] = s_o[warp + k][lane + 32 * j];
       add(s_ml[warp + k].x, s_ml[warp + k].y, o2);
     }
-    const int nd = idx / a.G, gh = idx - nd * a.G, h = d.y * a.G + gh;
+    const int nd = a.g_div(idx), gh = idx - nd * a.G, h = d.y * a.G + gh;
     const bool live = !(m == -INFINITY && l == 0.f);         // (a node in use sees itself)
     const float inv = live ? 1.f / l : 0.f;
     T* out = static_cast<T*>(a.out) + (int64_t)(r0 + nd) * a.out_row + (int64_t)h * DH;
