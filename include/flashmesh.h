@@ -446,7 +446,7 @@ int fm_device_status(fm_ctx* ctx);
 #define FM_MAX_TOP 32               /* alternatives per row of fm_logprobs                          */
 #define FM_MAX_TREE_NODES 256       /* nodes of one tree                                            */
 #define FM_MAX_SEQS 4096            /* sequences of one fm_pages, entries of one of its calls       */
-#define FM_MAX_TREES 1024           /* trees of one fm_tree_attention                               */
+#define FM_MAX_TREES 512            /* trees of one fm_tree_attention                               */
 
 /* A pool of cache pages: element i of the key of position `slot` of page `page`, head h, layer l is
  * k[l*layer_stride + page*page_stride + h*head_stride + slot*slot_stride + i]; values alike.  Strides

@@ -129,14 +129,14 @@ int score_rows(const lp::Args& a, cudaStream_t stream) {
   return launched();
 }
 
-// Rows that share keys (nodes x heads of a group): up to 16 take the warp-level form, more the tensor cores' tiles of 128.
+// Rows that share keys (nodes x heads of a group): up to 16 take the warp-level form, more the tensor cores' tiles of 256.
 inline bool few_rows(int max_nodes, int group) { return (int64_t)max_nodes * group <= 16; }
 using tr::DESC_BYTES;
-static_assert(DESC_BYTES >= 2 * tr::SMS * sizeof(int4), "");
-static_assert(tr::Rows16<128>::C == tr::Rows128<64>::C && tr::Rows16<128>::C == tr::Rows128<128>::C, "make_maps: one chunk for the three of them");
-static_assert(tr::Rows16<128>::FIXED + tr::plan_bytes(FM_MAX_TREES) <= 227 * 1024 && tr::Rows128<128>::FIXED + tr::plan_bytes(FM_MAX_TREES) <= 227 * 1024, "");
+static_assert(DESC_BYTES >= tr::SMS * sizeof(int4), "");
+static_assert(tr::Rows16<64>::C == 128 && tr::Rows256<64>::C == 128 && tr::Rows256<128>::C == 128 && tr::Rows16<128>::C == 64, "make_maps");
+static_assert(tr::Rows16<128>::FIXED + tr::plan_bytes(FM_MAX_TREES) <= 227 * 1024 && tr::Rows256<128>::FIXED + tr::plan_bytes(FM_MAX_TREES) <= 227 * 1024, "");
 inline size_t tree_bytes(bool few, int dh) {
-  return DESC_BYTES + (size_t)(few ? tr::SMS : 2 * tr::SMS) * 2 * (few ? 16 : 128) * (dh + 2) * sizeof(float);
+  return DESC_BYTES + (size_t)tr::SMS * 2 * (few ? 16 : 256) * (dh + 2) * sizeof(float);
 }
 
 typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
@@ -193,11 +193,11 @@ int tree_attention(const tr::Args& a, cudaStream_t stream) {
     if (!whole_for_sure(a, 16, CF::C, tr::SMS)) e = launch_behind(tr::merge_kernel<T, DH, 16>, dim3(tr::SMS, 4), 256, stream, a);
   } else {
     static std::atomic<uint64_t> asked{0};
-    using CF = tr::Rows128<DH>;
-    if (!allow_smem(tr::rows128_kernel<T, DH>, CF::bytes(FM_MAX_TREES), asked)) return FM_ERR_CUDA;
-    tr::rows128_kernel<T, DH><<<2 * tr::SMS, CF::THREADS, CF::bytes(a.batch), stream>>>(a);
+    using CF = tr::Rows256<DH>;
+    if (!allow_smem(tr::rows256_kernel<T, DH>, CF::bytes(FM_MAX_TREES), asked)) return FM_ERR_CUDA;
+    tr::rows256_kernel<T, DH><<<tr::SMS, CF::THREADS, CF::bytes(a.batch), stream>>>(a);
     if (cudaGetLastError() != cudaSuccess) return FM_ERR_CUDA;
-    if (!whole_for_sure(a, 128, CF::C, 2 * tr::SMS)) e = launch_behind(tr::merge_kernel<T, DH, 128>, dim3(2 * tr::SMS, 8), 256, stream, a);
+    if (!whole_for_sure(a, 256, CF::C, tr::SMS)) e = launch_behind(tr::merge_kernel<T, DH, 256>, dim3(tr::SMS, 16), 256, stream, a);
   }
   return e == cudaSuccess ? FM_OK : FM_ERR_CUDA;
 }
@@ -219,7 +219,7 @@ Div div_by(int d) {
 }
 size_t workspace_bytes(int max_nodes, int group, int head_dim) { return tree_bytes(few_rows(max_nodes, group), head_dim); }
 bool make_maps(const fm_cache& c, int layer, int max_pages, Args& a) {
-  return make_maps_of(c, layer, max_pages, few_rows(a.max_nodes, a.G) && c.head_dim == 64 ? Rows16<64>::C : Rows16<128>::C, a);
+  return make_maps_of(c, layer, max_pages, few_rows(a.max_nodes, a.G) && c.head_dim == 128 ? 64 : 128, a);
 }
 int launch(const Args& a, int dtype, int head_dim, cudaStream_t stream) {
   if (dtype == FM_BF16) return head_dim == 64 ? tree_attention<bf16, 64>(a, stream) : tree_attention<bf16, 128>(a, stream);

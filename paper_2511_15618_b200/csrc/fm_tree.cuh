@@ -1,7 +1,7 @@
 // Attention of trees of drafted tokens over a paged cache, and the walk that accepts a path.
 //
-// A tile is what shares keys: the query rows (nodes x heads of the group) of one sequence and kv-head, 16 or 128 of them.  Its keys
-// come in chunks of C: conditioning slots, the window's slots (or all cached ones), the nodes.  The launch is one or two CTAs
+// A tile is what shares keys: the query rows (nodes x heads of the group) of one sequence and kv-head, 16 or 256 of them.  Its keys
+// come in chunks of C: conditioning slots, the window's slots (or all cached ones), the nodes.  The launch is one CTA
 // per SM whatever the lengths: the chunks of all tiles, one tile after the other, are cut into equal shares (their total is
 // known on the device alone), so ragged batches are balanced without the host.  A cut falls inside a tile at most once per CTA; the
 // parts of a cut tile go to a scratch buffer and a second small launch merges them in order.
@@ -21,7 +21,7 @@
 
 namespace tr {
 
-constexpr int SMS = 148;                // of a B200: one CTA each (16-row tiles) or two (128); the workspace is laid out for them
+constexpr int SMS = 148;                // of a B200: one CTA each; the workspace is laid out for them
 constexpr int WORDS = FM_MAX_TREE_NODES / 32;
 
 struct Div {                            // division of 0 <= n < 2^31 by a constant
@@ -292,26 +292,31 @@ __device__ inline int parts_of(const Args& a, const Plan& p, int cta, long long 
 }
 
 // ---- loading, by a warp
-// A chunk of cached positions as TMA boxes, a lane each.  The page id is read ahead of the wait for a place in the ring.
+// A chunk of cached positions as TMA boxes, a lane each.  Page ids are read ahead of the wait for a place in the ring.
 // (Requests of a warp go out one after the other, some 75 ns each: several warps share a chunk's, one map or half each.)
-struct Box { int id, in_page; };                             // id -1: none
 template <int C>
-__device__ inline Box box_of(const Args& a, const Seq& s, const Chunk& k, int lane) {
-  const int rows = min(a.page_div.d, C), slot = place_of(a, k.start + lane * rows);        // (at most C / 8 = 16 boxes)
-  Box x{-1, 0};
-  if (!k.tree && lane * rows < k.n) {
-    const int pi = a.page_div(slot);
-    x.id = __ldg(a.table + (int64_t)s.seq * a.max_pages + pi);
+struct Ids {
+  int id[C / 32], in_page;              // of the lane's box: id[0] and its first slot in the page; of rows that are copied: row 32 j + lane.  -1: none
+};
+template <int C>
+__device__ inline void fetch_ids(const Args& a, const Seq& s, const Chunk& k, int lane, Ids<C>& x) {
+  if (k.tree) return;
+  const int* table = a.table + (int64_t)s.seq * a.max_pages;
+  if (boxed(a, k)) {
+    const int rows = min(a.page_div.d, C), slot = place_of(a, k.start + lane * rows), pi = a.page_div(slot);      // (at most C / 8 = 16 boxes)
+    x.id[0] = lane * rows < k.n ? __ldg(table + pi) : -1;
     x.in_page = slot - pi * a.page_div.d;
+  } else {
+#pragma unroll
+    for (int j = 0; j < C / 32; ++j) x.id[j] = 32 * j + lane < k.n ? __ldg(table + a.page_div(place_of(a, k.start + 32 * j + lane))) : -1;
   }
-  return x;
 }
 // boxes first, first + step, ... of 64 features from `x0` to `to` (rows of 128 bytes); every lane arrives on the barrier once
 template <int C>
-__device__ inline void request_boxes(const Args& a, const CUtensorMap* map, int x0, const Chunk& k, Box x, int first, int step, int hk, unsigned char* to,
+__device__ inline void request_boxes(const Args& a, const CUtensorMap* map, int x0, const Chunk& k, const Ids<C>& x, int first, int step, int hk, unsigned char* to,
                                      uint64_t* bar, int lane) {
   const int rows = min(a.page_div.d, C);
-  const bool mine = lane * rows < k.n && lane % step == first, ok = mine && x.id >= 0 && x.id < a.n_pages;
+  const bool mine = lane * rows < k.n && lane % step == first, ok = mine && x.id[0] >= 0 && x.id[0] < a.n_pages;
   if (mine && !ok) {                                         // no page: zeros, and the caller is told
     if (a.status != nullptr) atomicMin(a.status, FM_ERR_INVALID_ARG);
     for (int i = 0; i < rows * 8; ++i) reinterpret_cast<uint4*>(to + lane * rows * 128)[i] = make_uint4(0u, 0u, 0u, 0u);
@@ -320,19 +325,22 @@ __device__ inline void request_boxes(const Args& a, const CUtensorMap* map, int 
   const int n = __popc(__ballot_sync(0xffffffffu, ok));
   if (lane == 0) ptx::mbar_expect_tx(bar, (uint32_t)(n * rows * 128)); else ptx::mbar_arrive(bar);
   __syncwarp();
-  if (ok) ptx::tma_load_4d(to + lane * rows * 128, map, x0, x.in_page, hk, x.id, bar);
+  if (ok) ptx::tma_load_4d(to + lane * rows * 128, map, x0, x.in_page, hk, x.id[0], bar);
   __syncwarp();
 }
 // The same with 16-byte copies, also for nodes; what is not there is zero.  By `threads` threads, the calling one is `t`;
-// the copies are theirs (cp.async).  KV: 0 keys, 1 values, 2 both.
+// the copies are theirs (cp.async).  A warp's lanes share a group of 32 rows at a time.  KV: 0 keys, 1 values, 2 both.
 template <typename T, int DH, int C, int KV>
-__device__ inline void request_pieces(const Args& a, const Seq& s, const Chunk& k, int hk, unsigned char* Ks, unsigned char* Vs, int t, int threads) {
+__device__ inline void request_pieces(const Args& a, const Seq& s, const Chunk& k, int hk, unsigned char* Ks, unsigned char* Vs, const Ids<C>& x, int t, int threads) {
   constexpr int PIECES = DH / 8;
   const int piece = t % PIECES, step = threads / PIECES;
   const uint32_t ks = ptx::smem_u32(Ks) + (piece >> 3) * C * 128, vs = ptx::smem_u32(Vs) + (piece >> 3) * C * 128;
-  const int* table = a.table + (int64_t)s.seq * a.max_pages;
 #pragma unroll 4
   for (int r = t / PIECES; r < C; r += step) {
+    int group = x.id[0];
+#pragma unroll
+    for (int j = 1; j < C / 32; ++j) if (r >> 5 == j) group = x.id[j];
+    const int id = __shfl_sync(0xffffffffu, group, r & 31);
     bool there = r < k.n;
     const T *kp = reinterpret_cast<const T*>(a.k), *vp = reinterpret_cast<const T*>(a.v);
     int64_t at = 0;
@@ -340,7 +348,7 @@ __device__ inline void request_pieces(const Args& a, const Seq& s, const Chunk& 
       kp = static_cast<const T*>(a.k_new); vp = static_cast<const T*>(a.v_new);
       if (there) at = (int64_t)(s.r0 + k.start + r) * a.new_row + hk * DH;
     } else if (there) {
-      const int slot = place_of(a, k.start + r), pi = a.page_div(slot), id = __ldg(table + pi);
+      const int slot = place_of(a, k.start + r), pi = a.page_div(slot);
       if (id < 0 || id >= a.n_pages) {
         there = false;
         if (a.status != nullptr) atomicMin(a.status, FM_ERR_INVALID_ARG);
@@ -524,7 +532,8 @@ __global__ void __launch_bounds__(Rows16<DH>::THREADS, 1) rows16_kernel(const __
       cp_arrive(q_full + (part & 1));
       ++part;
       Chunk k = chunk_of<C>(w.s, w.c);
-      Box x = box_of<C>(a, w.s, k, lane);
+      Ids<C> x;
+      fetch_ids<C>(a, w.s, k, lane, x);
       for (int c = w.c; c < w.c_end; ++c, ++i) {
         const int st = i % ST;
         if (i >= ST && !(ok = wait(empty + st, ((i / ST) - 1) & 1))) break;
@@ -533,11 +542,11 @@ __global__ void __launch_bounds__(Rows16<DH>::THREADS, 1) rows16_kernel(const __
           if (written > 0) { --written; ptx::fence_proxy_async(); }
           request_boxes<C>(a, map, x0, k, x, first, step, hk, Ks + off, full + st, lane);
         } else {
-          request_pieces<T, DH, C, 2>(a, w.s, k, hk, Ks, Ks + CF::TILE, tid, 128);
+          request_pieces<T, DH, C, 2>(a, w.s, k, hk, Ks, Ks + CF::TILE, x, tid, 128);
           cp_arrive(full + st);
           written = ST;
         }
-        if (c + 1 < w.c_end) { k = chunk_of<C>(w.s, c + 1); x = box_of<C>(a, w.s, k, lane); }
+        if (c + 1 < w.c_end) { k = chunk_of<C>(w.s, c + 1); fetch_ids<C>(a, w.s, k, lane, x); }
       }
     }
     if (!ok) s_fail = 1;
@@ -803,22 +812,29 @@ __global__ void __launch_bounds__(Rows16<DH>::THREADS, 1) rows16_kernel(const __
 }
 
 // ------------------------------------------------------------------------------------------
-// 128 query rows a tile, on the tensor cores
+// 256 query rows a tile, on the tensor cores
 // ------------------------------------------------------------------------------------------
 // S = Q K^T and O += P V are tcgen05 MMAs with accumulators in tensor memory; V is multiplied as it lies (keys x features:
-// MN-major), P goes back to tensor memory as the A operand.  Two threads share a row of the softmax and exchange
-// maxima; S of the next chunk is multiplied as soon as S is in registers.  The output is rescaled only when a row's
-// maximum has grown by more than 2^8 (P then stays below 2^8).  Two CTAs per SM: one's softmax
-// runs under the other's MMAs.  One warp brings keys, one values, each as soon as its place is free (keys once their scores
-// are multiplied); a third one (the fixer) brings queries and takes values that are not finite out of chunks with hidden keys.  What
-// threads write is made visible to the tensor cores by a proxy fence.  P has two places: the exponentials of a chunk do
-// not wait for the product of the one before.
+// MN-major), P goes back to tensor memory as the A operand.  Two slots work in turn, each with its S, P and O and four warps
+// of softmax, a thread a row: one's exponentials run under the other's products.  A tile of more than 128 rows gives each slot
+// half of them and every chunk to both (keys and values are loaded once for 256 rows); one of up to 128 rows gives its
+// chunks to the slots alternately, and their outputs are merged at the end.  Steps are numbered through: slot = step mod 2.
+// The output is rescaled only when a row's maximum has grown by more than 2^8 (P then stays below 2^8).
+// One warp brings keys, one values, each as soon as its place is free (keys once their scores are multiplied); a third
+// one (the fixer) brings queries and takes values that are not finite out of chunks with hidden keys.  What threads write is
+// made visible to the tensor cores by a proxy fence.
+// Bound: the special-function units (1024 clocks for the exponentials of 128 rows x 128 keys, about what the products of
+// heads of 128 take), or, where a tile has few rows, memory.
 template <int DH>
-struct Rows128 {
-  static constexpr int ROWS = 128, C = 64, STAGES = DH == 64 ? 4 : 2, HC = C / 2;
-  static constexpr int THREADS = 96 + 256 + 32;              // keys, fixer, MMA, softmax, values
+struct Rows256 {
+  static constexpr int ROWS = 256, C = 128, STAGES = DH == 64 ? 4 : 2;
+  static constexpr int THREADS = 128 + 256;                  // keys, fixer, MMA, values; softmax
   static constexpr int Q = 128 * DH * 2, TILE = C * DH * 2, STAGE = 2 * TILE;
-  static constexpr int FIXED = Q + STAGES * STAGE + (int)sizeof(Tree) + 512 * 4 + 512 + 1024;
+  // tensor memory, columns: S of both slots, O of both; P of heads of 64 behind them, of heads of 128 in the place of S
+  static constexpr bool ALIAS = DH == 128;
+  static constexpr int O_AT = 2 * C, P_AT = O_AT + 2 * DH;
+  static_assert(P_AT + (ALIAS ? 0 : 2 * C / 2) <= 512, "");
+  static constexpr int FIXED = 2 * Q + STAGES * STAGE + (int)sizeof(Tree) + 2 * 128 * 8 + 512 + 1024;
   static int bytes(int batch) { return FIXED + plan_bytes(batch); }
 };
 constexpr float GROW = 8.f;
@@ -896,19 +912,19 @@ __device__ inline const T* values_of(const Args& a, const Seq& s, const Chunk& k
 }
 
 template <typename T, int DH>
-__global__ void __launch_bounds__(Rows128<DH>::THREADS, 2) rows128_kernel(const __grid_constant__ Args a) {
-  using CF = Rows128<DH>;
-  constexpr int C = CF::C, HC = CF::HC, ST = CF::STAGES, TILE = CF::TILE, STAGE = CF::STAGE;
+__global__ void __launch_bounds__(Rows256<DH>::THREADS, 1) rows256_kernel(const __grid_constant__ Args a) {
+  using CF = Rows256<DH>;
+  constexpr int C = CF::C, ST = CF::STAGES, TILE = CF::TILE, STAGE = CF::STAGE;
   extern __shared__ unsigned char smem_raw[];
   unsigned char* sm = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-  unsigned char* ring = sm + CF::Q;                          // behind the queries
-  float* s_pair = reinterpret_cast<float*>(ring + ST * STAGE);             // [use mod 2][half][row]
-  int4* s_info = reinterpret_cast<int4*>(s_pair + 512);
+  unsigned char* ring = sm + 2 * CF::Q;                      // behind the queries
+  float2* s_ml = reinterpret_cast<float2*>(ring + ST * STAGE);             // [slot][row] maxima and sums
+  int4* s_info = reinterpret_cast<int4*>(s_ml + 256);
   long long* s_base = reinterpret_cast<long long*>(s_info + a.batch);
   long long* s_sh = s_base + a.batch + 1;                    // [2 * warps]
   uint64_t* full = reinterpret_cast<uint64_t*>(s_sh + 24);
-  uint64_t *full_v = full + ST, *fixed = full_v + ST, *free_k = fixed + ST, *free_v = free_k + ST, *q_full = free_v + ST, *q_free = q_full + 1, *s_full = q_free + 1, *s_read = s_full + 1, *p_full = s_read + 1,
-           *o_full = p_full + 2, *done = o_full + 2;
+  uint64_t *full_v = full + ST, *fixed = full_v + ST, *free_k = fixed + ST, *free_v = free_k + ST, *q_full = free_v + ST, *q_free = q_full + 1,
+           *s_full = q_free + 1, *p_full = s_full + 2, *o_full = p_full + 2, *done = o_full + 2;           // (the last four: a slot each)
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(done + 1);
   Tree& tree = *reinterpret_cast<Tree*>(done + 2);
   int* s_tile_base = reinterpret_cast<int*>(&tree + 1);
@@ -921,27 +937,28 @@ __global__ void __launch_bounds__(Rows128<DH>::THREADS, 2) rows128_kernel(const 
       ptx::mbar_init(full + i, 32); ptx::mbar_init(full_v + i, 32); ptx::mbar_init(fixed + i, 32);
       ptx::mbar_init(free_k + i, 1); ptx::mbar_init(free_v + i, 1);
     }
-    ptx::mbar_init(q_full, 32); ptx::mbar_init(q_free, 1); ptx::mbar_init(s_full, 1); ptx::mbar_init(s_read, 8); ptx::mbar_init(p_full, 8); ptx::mbar_init(p_full + 1, 8);
-    ptx::mbar_init(o_full, 1); ptx::mbar_init(o_full + 1, 1); ptx::mbar_init(done, 1);
+    ptx::mbar_init(q_full, 32); ptx::mbar_init(q_free, 1); ptx::mbar_init(done, 1);
+    for (int i = 0; i < 2; ++i) { ptx::mbar_init(s_full + i, 1); ptx::mbar_init(p_full + i, 4); ptx::mbar_init(o_full + i, 1); }
     ptx::fence_mbar_init();
   }
   if (warp == 2) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(ptx::smem_u32(tmem_slot)), "r"(256) : "memory");
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(ptx::smem_u32(tmem_slot)), "r"(512) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   Plan plan;
-  make_plan<C, 128, CF::THREADS>(a, plan, s_info, s_base, s_tile_base, s_sh);
-  Walk<C, 128> w;
+  make_plan<C, 256, CF::THREADS>(a, plan, s_info, s_base, s_tile_base, s_sh);
+  Walk<C, 256> w;
   w.init(a, plan, blockIdx.x);
   tc::fence_before();
   __syncthreads();
   tc::fence_after();
-  const uint32_t tmem = ptx::uniform(*tmem_slot), tO = tmem + C, tP = tO + DH;             // S in columns 0 .. C-1, then O, then P twice
+  const uint32_t tmem = ptx::uniform(*tmem_slot);
   auto wait = [](uint64_t* bar, uint32_t parity) { return __all_sync(0xffffffffu, ptx::mbar_wait(bar, parity)) != 0; };
+  auto two = [&] { return w.s.n * a.G - w.mt * 256 > 128; };               // more than 128 rows in the tile
 
-  if (warp == 0 || warp == 11) {
+  if (warp == 0 || warp == 3) {
     // ---- keys, values
-    const bool v = warp == 11;
+    const bool v = warp == 3;
     uint64_t *mine = v ? full_v : full, *room = v ? free_v : free_k;
     int i = 0;
     int4 cut = make_int4(0, 0, 0, 0);
@@ -951,7 +968,8 @@ __global__ void __launch_bounds__(Rows128<DH>::THREADS, 2) rows128_kernel(const 
       const int hk = w.hk;
       if (w.starts() && !w.ends()) { cut = make_int4(w.b, hk, w.mt, 1); cut_end = w.tile_start + w.s.chunks + OVER; }
       Chunk k = chunk_of<C>(w.s, w.c);
-      Box x = box_of<C>(a, w.s, k, lane);
+      Ids<C> x;
+      fetch_ids<C>(a, w.s, k, lane, x);
       for (int c = w.c; c < w.c_end; ++c, ++i) {
         const int st = i % ST;
         unsigned char *Ks = ring + st * STAGE, *Vs = Ks + TILE;
@@ -960,7 +978,7 @@ __global__ void __launch_bounds__(Rows128<DH>::THREADS, 2) rows128_kernel(const 
           // (both halves of a box in a lane: they land on one barrier, which every lane arrives on once)
           const CUtensorMap* map = v ? &a.map_v : &a.map_k;
           const int rows = min(a.page_div.d, C);
-          const bool has = lane * rows < k.n, good = has && x.id >= 0 && x.id < a.n_pages;
+          const bool has = lane * rows < k.n, good = has && x.id[0] >= 0 && x.id[0] < a.n_pages;
           unsigned char* to = (v ? Vs : Ks) + lane * rows * 128;
           if (has && !good) {                                // no page: zeros, and the caller is told
             if (a.status != nullptr) atomicMin(a.status, FM_ERR_INVALID_ARG);
@@ -973,29 +991,29 @@ __global__ void __launch_bounds__(Rows128<DH>::THREADS, 2) rows128_kernel(const 
           __syncwarp();
           if (good) {
 #pragma unroll
-            for (int h = 0; h < DH / 64; ++h) ptx::tma_load_4d(to + h * C * 128, map, h * 64, x.in_page, hk, x.id, mine + st);
+            for (int h = 0; h < DH / 64; ++h) ptx::tma_load_4d(to + h * C * 128, map, h * 64, x.in_page, hk, x.id[0], mine + st);
           }
           __syncwarp();
         } else {
-          if (v) request_pieces<T, DH, C, 1>(a, w.s, k, hk, Ks, Vs, lane, 32); else request_pieces<T, DH, C, 0>(a, w.s, k, hk, Ks, Vs, lane, 32);
+          if (v) request_pieces<T, DH, C, 1>(a, w.s, k, hk, Ks, Vs, x, lane, 32); else request_pieces<T, DH, C, 0>(a, w.s, k, hk, Ks, Vs, x, lane, 32);
           asm volatile("cp.async.wait_all;" ::: "memory");
           ptx::fence_proxy_async();
           ptx::mbar_arrive(mine + st);
         }
-        if (c + 1 < w.c_end) { k = chunk_of<C>(w.s, c + 1); x = box_of<C>(a, w.s, k, lane); }
+        if (c + 1 < w.c_end) { k = chunk_of<C>(w.s, c + 1); fetch_ids<C>(a, w.s, k, lane, x); }
       }
     }
     if (!ok) s_fail = 1;
-    if (!v) write_desc<C, 128>(a, plan, cut, cut_end, lane);
+    if (!v) write_desc<C, 256>(a, plan, cut, cut_end, lane);
   } else if (warp == 1) {
     // ---- fixing
     int i = 0, part = 0;
     bool ok = true;
     while (ok && w.next(a, plan)) {
-      const int hk = w.hk;
       // the tile's queries, once the scores of the tile before have been multiplied
       if (part > 0 && !(ok = wait(q_free, (part - 1) & 1))) break;
-      request_queries<T, DH, 128>(a, w.s, hk, w.mt, sm, lane, 32);
+      request_queries<T, DH, 128>(a, w.s, w.hk, 2 * w.mt, sm, lane, 32);
+      if (two()) request_queries<T, DH, 128>(a, w.s, w.hk, 2 * w.mt + 1, sm + CF::Q, lane, 32);
       asm volatile("cp.async.wait_all;" ::: "memory");
       ptx::fence_proxy_async();
       ptx::mbar_arrive(q_full);
@@ -1023,159 +1041,209 @@ __global__ void __launch_bounds__(Rows128<DH>::THREADS, 2) rows128_kernel(const 
     if (!ok) s_fail = 1;
     asm volatile("cp.async.wait_all;" ::: "memory");
   } else if (warp == 2) {
-    // ---- multiplying
+    // ---- multiplying.  Scores run two steps ahead of the products with values, inside a tile.
     const uint32_t id_s = instr_desc<T>(C), id_o = instr_desc<T>(64) | (1u << 16);          // B of P V is MN-major
     const uint64_t dq = tc::smem_desc_sw128(ptx::smem_u32(sm));
-    int it = 0;
+    int g = 0, it = 0, part = 0;                             // step, chunk of the ring, tile
     bool ok = true;
-    int part = 0;
-    auto scores = [&](int i, bool first, bool last) {
-      const int st = i % ST;
-      if (first && !wait(q_full, part++ & 1)) return false;
-      if (!wait(full + st, (i / ST) & 1)) return false;
-      tc::fence_after();
-      const uint64_t dk = tc::smem_desc_sw128(ptx::smem_u32(ring + st * STAGE));
-      if (ptx::elect_one()) {
+    while (ok && w.next(a, plan)) {
+      const int per = two() ? 2 : 1, steps = (w.c_end - w.c) * per;        // steps a chunk, steps of the tile
+      if (!(ok = wait(q_full, part++ & 1))) break;
+      auto scores = [&](int k) {                             // step k of the tile
+        const int i = it + k / per, st = i % ST, slot = (g + k) & 1, sub = per == 2 ? k & 1 : 0;
+        const bool first_of = per == 1 || sub == 0, last_of = per == 1 || sub == 1;
+        if (first_of && !wait(full + st, (i / ST) & 1)) return false;
+        // the slot's last product has read P where the scores go (heads of 128), its last softmax the scores
+        if (CF::ALIAS && g + k >= 2 && !wait(o_full + slot, ((g + k - 2) >> 1) & 1)) return false;
+        tc::fence_after();
+        const uint64_t q = dq + sub * (CF::Q / 16), dk = tc::smem_desc_sw128(ptx::smem_u32(ring + st * STAGE));
+        if (ptx::elect_one()) {
 #pragma unroll
-        for (int k = 0; k < DH / 16; ++k)                    // 64 features a half, 16 a step
-          tc::mma_ss(tmem, dq + (k >> 2) * (128 * 128 / 16) + 2 * (k & 3), dk + (k >> 2) * (C * 128 / 16) + 2 * (k & 3), id_s, k > 0 ? 1u : 0u);
-        tc::commit(s_full);
-        tc::commit(free_k + st);
-        if (last) tc::commit(q_free);
+          for (int j = 0; j < DH / 16; ++j)                  // 64 features a half, 16 a step
+            tc::mma_ss(tmem + slot * C, q + (j >> 2) * (128 * 128 / 16) + 2 * (j & 3), dk + (j >> 2) * (C * 128 / 16) + 2 * (j & 3), id_s, j > 0 ? 1u : 0u);
+          tc::commit(s_full + slot);
+          if (last_of) tc::commit(free_k + st);
+          if (k == steps - 1) tc::commit(q_free);
+        }
+        return true;
+      };
+      ok = scores(0) && (steps < 2 || scores(1));
+      for (int k = 0; k < steps && ok; ++k) {
+        const int i = it + k / per, st = i % ST, slot = (g + k) & 1, sub = per == 2 ? k & 1 : 0;
+        if (sub == 0 && !(ok = wait(full_v + st, (i / ST) & 1) && wait(fixed + st, (i / ST) & 1))) break;
+        if (!(ok = wait(p_full + slot, ((g + k) >> 1) & 1))) break;
+        tc::fence_after();
+        const uint64_t dv = tc::smem_desc_sw128(ptx::smem_u32(ring + st * STAGE + TILE));
+        const uint32_t tO = tmem + CF::O_AT + slot * DH, tP = tmem + (CF::ALIAS ? slot * C : CF::P_AT + slot * C / 2);
+        const bool fresh = k < 2;                            // the slot's first product of the tile
+        if (ptx::elect_one()) {
+#pragma unroll
+          for (int h = 0; h < DH / 64; ++h)
+#pragma unroll
+            for (int j = 0; j < C / 16; ++j) mma_ts(tO + 64 * h, tP + 8 * j, dv + h * (C * 128 / 16) + 128 * j, id_o, (!fresh || j > 0) ? 1u : 0u);
+          tc::commit(o_full + slot);
+          if (per == 1 || sub == 1) tc::commit(free_v + st);
+        }
+        if (k + 2 < steps) ok = scores(k + 2);
       }
-      return true;
-    };
-    bool more = w.next(a, plan);
-    int c = w.c;
-    if (more) ok = scores(0, true, c + 1 == w.c_end);
-    while (more && ok) {
-      const bool first = c == w.c, last = c + 1 == w.c_end;
-      const int st = it % ST;
-      if (!(ok = wait(s_read, it & 1))) break;
-      if (last) { more = w.next(a, plan); c = w.c; } else { ++c; }
-      if (more && !(ok = scores(it + 1, last, c + 1 == w.c_end))) break;
-      if (!(ok = wait(full_v + st, (it / ST) & 1) && wait(fixed + st, (it / ST) & 1) && wait(p_full + (it & 1), (it >> 1) & 1))) break;
-      tc::fence_after();
-      const uint64_t dv = tc::smem_desc_sw128(ptx::smem_u32(ring + st * STAGE + TILE));
-      if (ptx::elect_one()) {
-#pragma unroll
-        for (int h = 0; h < DH / 64; ++h)
-#pragma unroll
-          for (int k = 0; k < C / 16; ++k) mma_ts(tO + 64 * h, tP + 32 * (it & 1) + 8 * k, dv + h * (C * 128 / 16) + 128 * k, id_o, (!first || k > 0) ? 1u : 0u);
-        tc::commit(free_v + st);
-        tc::commit(o_full + (it & 1));
-      }
-      ++it;
+      g += steps;
+      it += w.c_end - w.c;
     }
     if (!ok) s_fail = 1;
     if (ptx::elect_one()) tc::commit(done);                  // what was issued ends before the CTA does
     wait(done, 0);
   } else {
-    // ---- softmax: warps w and w + 4 share 32 query rows, half of a chunk's keys each
-    const int w4 = warp & 3, half = (warp - 3) >> 2, i_row = w4 * 32 + lane, tid = threadIdx.x - 96;
-    const uint32_t lanes = (uint32_t)(w4 * 32) << 16;
-    auto sync = [] { asm volatile("bar.sync 5, 256;" ::: "memory"); };
-    auto meet = [&] { asm volatile("bar.sync %0, 64;" ::"r"(1 + w4) : "memory"); };
+    // ---- softmax: a slot's four warps, a thread a row
+    const int w4 = warp & 3, slot = (warp - 4) >> 2, i_row = w4 * 32 + lane, tid = threadIdx.x - 128;
+    const uint32_t lanes = (uint32_t)(w4 * 32) << 16, tS = tmem + slot * C + lanes, tO = tmem + CF::O_AT + slot * DH + lanes,
+                   tP = CF::ALIAS ? tS : tmem + CF::P_AT + slot * C / 2 + lanes;
+    auto sync = [] { asm volatile("bar.sync 1, 256;" ::: "memory"); };
     const float sc = a.scale_log2;
-    int tree_of = -1, it = 0, x = 0;
+    int tree_of = -1, g = 0;
     bool ok = true;
     while (w.next(a, plan)) {
       const Seq& s = w.s;
-      const int hk = w.hk, mt = w.mt, idx = mt * 128 + i_row, M = s.n * a.G;
+      const bool both = two();                               // two tiles of rows, or two shares of the chunks
+      const int per = both ? 2 : 1, steps = (w.c_end - w.c) * per, k_first = (g + slot) & 1;               // the slot's first step of the tile: 0 or 1
+      const int hk = w.hk, idx = w.mt * 256 + (both ? k_first * 128 : 0) + i_row, M = s.n * a.G;
       if (tree_of != w.b) { build_tree<256>(tree, a.parent + s.r0, s.n, tid, sync); tree_of = w.b; }
-      const bool whole = w.starts() && w.ends();
-      const bool there = idx < M;
+      const bool whole = w.starts() && w.ends(), there = idx < M;
       const int node = there ? a.g_div(idx) : 0, gh = there ? idx - node * a.G : 0, depth = there ? tree.depth[node] : 0;
       const int low = a.window > 0 ? s.len + depth - a.window + 1 : 0, low_all = a.window > 0 ? s.len + tree.max_depth - a.window + 1 : 0;
-      float m = -INFINITY, l = 0.f;                          // the maximum in use (times scale, base 2), this half's sum
-      for (int c = w.c; c < w.c_end; ++c, ++it) {
-        const Chunk ck = chunk_of<C>(s, c);
-        const bool first = c == w.c;
+      float m = -INFINITY, l = 0.f;                          // the maximum in use (times scale, base 2), the sum
+      bool any = false;
+      for (int k = k_first; k < steps; k += 2) {
+        const Chunk ck = chunk_of<C>(s, w.c + k / per);
+        const int n = (g + k) >> 1;                          // the slot's step
         const bool all_vis = !ck.tree && ck.n == C && !(a.window > 0 && ck.start + C > a.n_prefix && ck.start < low_all);
-        ok = ok && wait(s_full, it & 1);                     // (goes on: its partner waits at the barrier)
+        ok = ok && wait(s_full + slot, n & 1);               // (goes on: the warps meet at barriers)
         tc::fence_after();
-        uint32_t r[HC];
-#pragma unroll
-        for (int j = 0; j < HC; j += 32) ld32(tmem + lanes + HC * half + j, r + j);
-        ld_wait();
-        tc::fence_before();
-        __syncwarp();
-        if (lane == 0) ptx::mbar_arrive(s_read);
+        uint32_t bits[C / 32];
         if (!all_vis) {
-          const uint32_t bits = seen(a, tree, ck, there ? node : -1, depth, low, HC * half);
 #pragma unroll
-          for (int j = 0; j < HC; ++j)
-            if (!((bits >> j) & 1u)) r[j] = 0xff800000u;     // -inf: exponential 0
+          for (int q = 0; q < C / 32; ++q) bits[q] = seen(a, tree, ck, there ? node : -1, depth, low, 32 * q);
         }
+        // pass one: the row's maximum
+        uint32_t r[2][32];
         float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+        ld32(tS, r[0]);
 #pragma unroll
-        for (int j = 0; j < HC; j += 8)
+        for (int q = 0; q < C / 32; ++q) {
+          ld_wait();
+          if (q + 1 < C / 32) ld32(tS + 32 * (q + 1), r[(q + 1) & 1]);
+          uint32_t* x = r[q & 1];
+          if (!all_vis) {
 #pragma unroll
-          for (int k = 0; k < 4; ++k) m4[k] = max3(m4[k], __uint_as_float(r[j + 2 * k]), __uint_as_float(r[j + 2 * k + 1]));
-        float mx = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * sc;
-        float* pair = s_pair + (x++ & 1) * 256;              // (two of them: written again behind the next use's barrier)
-        pair[half * 128 + i_row] = mx;
-        meet();
-        mx = fmaxf(mx, pair[(half ^ 1) * 128 + i_row]);
-        // P of the chunk two before has been multiplied: its place is free (behind the first chunks of the launch)
-        if (it >= 2) ok = ok && wait(o_full + (it & 1), ((it >> 1) - 1) & 1);
+            for (int j = 0; j < 32; ++j)
+              if (!((bits[q] >> j) & 1u)) x[j] = 0xff800000u;              // -inf: exponential 0
+          }
+#pragma unroll
+          for (int j = 0; j < 32; j += 8)
+#pragma unroll
+            for (int u = 0; u < 4; ++u) m4[u] = max3(m4[u], __uint_as_float(x[j + 2 * u]), __uint_as_float(x[j + 2 * u + 1]));
+        }
+        ld32(tS, r[0]);                                      // (under what follows)
+        const float mx = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * sc;
+        // the slot's last product is in: P's place, and O, are free
+        if (any) ok = ok && wait(o_full + slot, (n - 1) & 1);
         tc::fence_after();
         const bool grow = mx > m + GROW || (m == -INFINITY && mx != -INFINITY);
         if (__any_sync(0xffffffffu, grow)) {
           const float mn = grow ? mx : m, f = m == -INFINITY ? (grow ? 0.f : 1.f) : ex2(m - mn);
           m = mn;
           l *= f;
-          if (!first) {                                      // this half's columns of the output, once the chunk before is in
-            ok = ok && wait(o_full + ((it - 1) & 1), ((it - 1) >> 1) & 1);
-            tc::fence_after();
+          if (any) {
 #pragma unroll 1
-            for (int j = 0; j < DH / 2; j += 16) {
+            for (int j = 0; j < DH; j += 16) {
               uint32_t o[16];
-              tc::ld16(tO + lanes + DH / 2 * half + j, o);
+              tc::ld16(tO + j, o);
 #pragma unroll
-              for (int k = 0; k < 16; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * f);
-              st16(tO + lanes + DH / 2 * half + j, o);
+              for (int u = 0; u < 16; ++u) o[u] = __float_as_uint(__uint_as_float(o[u]) * f);
+              st16(tO + j, o);
             }
           }
         }
+        any = true;
         const float base = m == -INFINITY ? 0.f : m;
         const uint64_t nb = pack2(-base, -base), s2 = pack2(sc, sc);
         uint64_t sum[2] = {0ull, 0ull};
+        // pass two: exponentials.  (P of heads of 128 replaces scores that have been read: columns 16 q .. behind columns .. 32 q + 31.)
 #pragma unroll
-        for (int j = 0; j < HC; j += 32) {
+        for (int q = 0; q < C / 32; ++q) {
+          ld_wait();
+          if (q + 1 < C / 32) ld32(tS + 32 * (q + 1), r[(q + 1) & 1]);
+          uint32_t* x = r[q & 1];
+          if (!all_vis) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j)
+              if (!((bits[q] >> j) & 1u)) x[j] = 0xff800000u;
+          }
           uint32_t pk[16];
 #pragma unroll
-          for (int k = 0; k < 16; ++k) {
-            const float2 d = unpack2(fma2(pack2(__uint_as_float(r[j + 2 * k]), __uint_as_float(r[j + 2 * k + 1])), s2, nb));
+          for (int u = 0; u < 16; ++u) {
+            const float2 d = unpack2(fma2(pack2(__uint_as_float(x[2 * u]), __uint_as_float(x[2 * u + 1])), s2, nb));
             const float e0 = ex2(d.x), e1 = ex2(d.y);
-            sum[k & 1] = add2(sum[k & 1], pack2(e0, e1));
-            pk[k] = pack(e0, e1, T());
+            sum[u & 1] = add2(sum[u & 1], pack2(e0, e1));
+            pk[u] = pack(e0, e1, T());
           }
-          st16(tP + 32 * (it & 1) + lanes + (HC * half + j) / 2, pk);
+          st16(tP + 16 * q, pk);
         }
         const float2 sa = unpack2(sum[0]), sb = unpack2(sum[1]);
         l += (sa.x + sa.y) + (sb.x + sb.y);
         st_wait();
         tc::fence_before();
         __syncwarp();
-        if (lane == 0) ptx::mbar_arrive(p_full + (it & 1));
+        if (lane == 0) ptx::mbar_arrive(p_full + slot);
       }
-      float* pair = s_pair + (x++ & 1) * 256;
-      pair[half * 128 + i_row] = l;
-      meet();
-      l += pair[(half ^ 1) * 128 + i_row];
-      ok = ok && wait(o_full + ((it - 1) & 1), ((it - 1) >> 1) & 1);
-      tc::fence_after();
+      if (any) {
+        const int last = steps - 1 - ((steps - 1 - k_first) & 1);
+        ok = ok && wait(o_full + slot, ((g + last) >> 1) & 1);
+        tc::fence_after();
+      }
+      g += steps;
+      // ---- the rows' outputs: of two tiles each slot its own; of two shares each slot half the columns, out of both
+      float f_mine = 1.f, f_other = 0.f;
+      bool other = false;
+      int j_lo = 0, j_hi = DH;
+      if (!both) {
+        s_ml[slot * 128 + i_row] = make_float2(m, l);
+        tc::fence_before();
+        sync();
+        tc::fence_after();
+        const float2 q = s_ml[(slot ^ 1) * 128 + i_row];
+        other = steps > 1;                                   // (the other slot had a step)
+        const float mm = fmaxf(m, q.x);
+        // (no chunk on one side: maximum -inf and sum 0; a sum that is no number goes through)
+        f_mine = !any ? 0.f : (m == -INFINITY ? 1.f : ex2(m - mm));
+        f_other = !(other || !any) ? 0.f : (q.x == -INFINITY ? 1.f : ex2(q.x - mm));
+        other = other || !any;
+        l = (f_mine == 0.f ? 0.f : l * f_mine) + (f_other == 0.f ? 0.f : q.y * f_other);
+        m = mm;
+        j_lo = slot * (DH / 2); j_hi = j_lo + DH / 2;
+      }
       const bool live = there && tree.reach[node][node >> 5] != 0u;
       const float inv = live ? 1.f / l : 0.f;
+      const uint32_t tOther = tmem + CF::O_AT + (slot ^ 1) * DH + lanes;
       T* op = static_cast<T*>(a.out) + (int64_t)(s.r0 + node) * a.out_row + (hk * a.G + gh) * DH;
-      float* part = a.part + ((size_t)(blockIdx.x * 2 + (w.starts() ? 1 : 0)) * 128 + i_row) * (DH + 2);
+      float* part = a.part + ((size_t)(blockIdx.x * 2 + (w.starts() ? 1 : 0)) * 256 + (idx - w.mt * 256)) * (DH + 2);
 #pragma unroll 1
-      for (int j0 = DH / 2 * half; j0 < DH / 2 * (half + 1); j0 += 32) {
+      for (int j0 = j_lo; j0 < j_hi; j0 += 32) {
         uint32_t o[32];
         __syncwarp();
-        ld32(tO + lanes + j0, o);
-        ld_wait();
+        if (any) {
+          ld32(tO + j0, o);
+          ld_wait();
+        }
+#pragma unroll
+        for (int j = 0; j < 32; ++j) o[j] = f_mine == 0.f ? 0u : __float_as_uint(__uint_as_float(o[j]) * f_mine);
+        if (other) {
+          uint32_t u[32];
+          ld32(tOther + j0, u);
+          ld_wait();
+#pragma unroll
+          for (int j = 0; j < 32; ++j)
+            if (f_other != 0.f) o[j] = __float_as_uint(__uint_as_float(o[j]) + __uint_as_float(u[j]) * f_other);
+        }
         if (*reinterpret_cast<volatile int*>(&s_bad) != 0 && there) {
           // values that are not finite, for the rows that see their key (p > 0)
           for (int c = w.c; c < w.c_end; ++c) {
@@ -1214,11 +1282,12 @@ __global__ void __launch_bounds__(Rows128<DH>::THREADS, 2) rows128_kernel(const 
             *reinterpret_cast<float2*>(part + j0 + j) = live ? make_float2(__uint_as_float(o[j]), __uint_as_float(o[j + 1])) : make_float2(0.f, 0.f);
         }
       }
-      if (ok && there && half == 0) {
+      if (ok && there && (both || slot == 0)) {
         if (!whole) *reinterpret_cast<float2*>(part + DH) = live ? make_float2(m, l) : make_float2(-INFINITY, 0.f);
         else if (a.lse != nullptr) a.lse[(int64_t)(s.r0 + node) * a.H + hk * a.G + gh] = live ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
       }
-      tc::fence_before();                                    // (O is read: the next tile's first product, behind this warp's p_full, may replace it)
+      tc::fence_before();                                    // (O is read: the next tile's first product, behind p_full, may replace it)
+      if (!both) sync();                                     // (by both slots' warps)
     }
     if (!ok) s_fail = 1;
   }
@@ -1230,7 +1299,7 @@ __global__ void __launch_bounds__(Rows128<DH>::THREADS, 2) rows128_kernel(const 
     if (threadIdx.x == 0 && a.status != nullptr) atomicMin(a.status, FM_ERR_TIMEOUT);
     ptx::drain_delay();
   }
-  if (warp == 2) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(256) : "memory");
+  if (warp == 2) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
 }
 
 // ---- parts of the tiles that were cut, merged in order: grid (CTAs, blocks per tile); two, four or eight warps a row, by the number of
@@ -1353,7 +1422,7 @@ static __global__ void __launch_bounds__(128) accept_kernel(const int* tokens, c
   if (lane == 0) { n_acc[b] = at; next_tok[b] = at > 0 ? next : -1; }
 }
 
-constexpr size_t DESC_BYTES = 8192;      // in front of a workspace's parts: what the merge has to do, of up to 2 * SMS CTAs
+constexpr size_t DESC_BYTES = 8192;      // in front of a workspace's parts: what the merge has to do, of the CTAs
 // Launches, for the entry points and for the context's own passes (fm_ops.cu).
 size_t workspace_bytes(int max_nodes, int group, int head_dim);
 bool make_maps(const fm_cache& c, int layer, int max_pages, Args& a);          // a.max_nodes and a.G are set

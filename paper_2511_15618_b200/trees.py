@@ -19,7 +19,7 @@ FM_BF16, FM_FP16, FM_FP32 = 0, 1, 2
 FM_MAX_TOP = 32
 FM_MAX_TREE_NODES = 256
 FM_MAX_SEQS = 4096
-FM_MAX_TREES = 1024
+FM_MAX_TREES = 512
 
 
 class FmCache(C.Structure):
