@@ -819,7 +819,10 @@ __global__ void __launch_bounds__(Rows16<DH>::THREADS, 1) rows16_kernel(const __
 // of softmax, a thread a row: one's exponentials run under the other's products.  A tile of more than 128 rows gives each slot
 // half of them and every chunk to both (keys and values are loaded once for 256 rows); one of up to 128 rows gives its
 // chunks to the slots alternately, and their outputs are merged at the end.  Steps are numbered through: slot = step mod 2.
-// The output is rescaled only when a row's maximum has grown by more than 2^8 (P then stays below 2^8).
+// Exponentials are taken to the maximum in use, that of the row's first chunk, and the scores' maximum beside them: only when it
+// exceeds the one in use by more than P's type holds (2^40 for bfloat16, 2^12 for half) the output is rescaled and the
+// chunk's exponentials are taken again.  (The maximum first, then the exponentials: a step of a slot took 4200 clocks, 560
+// of them for the maximum.)
 // One warp brings keys, one values, each as soon as its place is free (keys once their scores are multiplied); a third
 // one (the fixer) brings queries and takes values that are not finite out of chunks with hidden keys.  What threads write is
 // made visible to the tensor cores by a proxy fence.
@@ -837,7 +840,7 @@ struct Rows256 {
   static constexpr int FIXED = 2 * Q + STAGES * STAGE + (int)sizeof(Tree) + 2 * 128 * 8 + 512 + 1024;
   static int bytes(int batch) { return FIXED + plan_bytes(batch); }
 };
-constexpr float GROW = 8.f;
+template <typename T> constexpr float HEADROOM = __is_same(T, bf16) ? 40.f : 12.f;      // log2 of what P may grow to
 
 __device__ inline uint64_t pack2(float a, float b) {
   uint64_t r;
@@ -1061,7 +1064,7 @@ __global__ void __launch_bounds__(Rows256<DH>::THREADS, 1) rows256_kernel(const 
 #pragma unroll
           for (int j = 0; j < DH / 16; ++j)                  // 64 features a half, 16 a step
             tc::mma_ss(tmem + slot * C, q + (j >> 2) * (128 * 128 / 16) + 2 * (j & 3), dk + (j >> 2) * (C * 128 / 16) + 2 * (j & 3), id_s, j > 0 ? 1u : 0u);
-          tc::commit(s_full + slot);
+          tc::commit(s_full + slot);                         // (counts when all that was issued before is done: the slot's last product too)
           if (last_of) tc::commit(free_k + st);
           if (k == steps - 1) tc::commit(q_free);
         }
@@ -1123,12 +1126,8 @@ __global__ void __launch_bounds__(Rows256<DH>::THREADS, 1) rows256_kernel(const 
 #pragma unroll
           for (int q = 0; q < C / 32; ++q) bits[q] = seen(a, tree, ck, there ? node : -1, depth, low, 32 * q);
         }
-        // pass one: the row's maximum
-        uint32_t r[2][32];
-        float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-        ld32(tS, r[0]);
-#pragma unroll
-        for (int q = 0; q < C / 32; ++q) {
+        uint32_t r[2][32], pk[CF::ALIAS ? C / 32 : 1][16];
+        auto block = [&](int q) -> uint32_t* {               // columns 32 q .. of the scores; the next ones are requested
           ld_wait();
           if (q + 1 < C / 32) ld32(tS + 32 * (q + 1), r[(q + 1) & 1]);
           uint32_t* x = r[q & 1];
@@ -1137,19 +1136,49 @@ __global__ void __launch_bounds__(Rows256<DH>::THREADS, 1) rows256_kernel(const 
             for (int j = 0; j < 32; ++j)
               if (!((bits[q] >> j) & 1u)) x[j] = 0xff800000u;              // -inf: exponential 0
           }
+          return x;
+        };
+        float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+        auto largest4 = [&](const uint32_t* x) {
 #pragma unroll
           for (int j = 0; j < 32; j += 8)
 #pragma unroll
             for (int u = 0; u < 4; ++u) m4[u] = max3(m4[u], __uint_as_float(x[j + 2 * u]), __uint_as_float(x[j + 2 * u + 1]));
+        };
+        auto row_max = [&] { return fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * sc; };
+        if (!any) {                                          // the row's first chunk: its maximum first
+          ld32(tS, r[0]);
+#pragma unroll
+          for (int q = 0; q < C / 32; ++q) largest4(block(q));
+          m = row_max();
         }
-        ld32(tS, r[0]);                                      // (under what follows)
-        const float mx = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * sc;
-        // the slot's last product is in: P's place, and O, are free
-        if (any) ok = ok && wait(o_full + slot, (n - 1) & 1);
-        tc::fence_after();
-        const bool grow = mx > m + GROW || (m == -INFINITY && mx != -INFINITY);
-        if (__any_sync(0xffffffffu, grow)) {
-          const float mn = grow ? mx : m, f = m == -INFINITY ? (grow ? 0.f : 1.f) : ex2(m - mn);
+        float sum;
+        while (true) {
+          const float base = m == -INFINITY ? 0.f : m;
+          const uint64_t nb = pack2(-base, -base), s2 = pack2(sc, sc);
+          uint64_t sums[2] = {0ull, 0ull};
+          ld32(tS, r[0]);
+#pragma unroll
+          for (int q = 0; q < C / 32; ++q) {
+            const uint32_t* x = block(q);
+            largest4(x);
+            uint32_t(&p)[16] = pk[CF::ALIAS ? q : 0];
+#pragma unroll
+            for (int u = 0; u < 16; ++u) {
+              const float2 d = unpack2(fma2(pack2(__uint_as_float(x[2 * u]), __uint_as_float(x[2 * u + 1])), s2, nb));
+              const float e0 = ex2(d.x), e1 = ex2(d.y);
+              sums[u & 1] = add2(sums[u & 1], pack2(e0, e1));
+              p[u] = pack(e0, e1, T());
+            }
+            if (!CF::ALIAS) st16(tP + 16 * q, p);
+          }
+          const float2 sa = unpack2(sums[0]), sb = unpack2(sums[1]);
+          sum = (sa.x + sa.y) + (sb.x + sb.y);
+          const float mx = row_max();
+          const bool over = mx > m + HEADROOM<T> || (m == -INFINITY && mx != -INFINITY);
+          if (!__any_sync(0xffffffffu, over)) break;
+          // seldom: rescale to the new maximum (the scores' arrival says that the slot's last product is in) and again
+          const float mn = over ? mx : m, f = m == -INFINITY ? (over ? 0.f : 1.f) : ex2(m - mn);
           m = mn;
           l *= f;
           if (any) {
@@ -1164,32 +1193,12 @@ __global__ void __launch_bounds__(Rows256<DH>::THREADS, 1) rows256_kernel(const 
           }
         }
         any = true;
-        const float base = m == -INFINITY ? 0.f : m;
-        const uint64_t nb = pack2(-base, -base), s2 = pack2(sc, sc);
-        uint64_t sum[2] = {0ull, 0ull};
-        // pass two: exponentials.  (P of heads of 128 replaces scores that have been read: columns 16 q .. behind columns .. 32 q + 31.)
+        l += sum;
+        // (P of heads of 128 goes where the scores are, when they are no longer needed)
+        if (CF::ALIAS) {
 #pragma unroll
-        for (int q = 0; q < C / 32; ++q) {
-          ld_wait();
-          if (q + 1 < C / 32) ld32(tS + 32 * (q + 1), r[(q + 1) & 1]);
-          uint32_t* x = r[q & 1];
-          if (!all_vis) {
-#pragma unroll
-            for (int j = 0; j < 32; ++j)
-              if (!((bits[q] >> j) & 1u)) x[j] = 0xff800000u;
-          }
-          uint32_t pk[16];
-#pragma unroll
-          for (int u = 0; u < 16; ++u) {
-            const float2 d = unpack2(fma2(pack2(__uint_as_float(x[2 * u]), __uint_as_float(x[2 * u + 1])), s2, nb));
-            const float e0 = ex2(d.x), e1 = ex2(d.y);
-            sum[u & 1] = add2(sum[u & 1], pack2(e0, e1));
-            pk[u] = pack(e0, e1, T());
-          }
-          st16(tP + 16 * q, pk);
+          for (int q = 0; q < C / 32; ++q) st16(tP + 16 * q, pk[q]);
         }
-        const float2 sa = unpack2(sum[0]), sb = unpack2(sum[1]);
-        l += (sa.x + sa.y) + (sb.x + sb.y);
         st_wait();
         tc::fence_before();
         __syncwarp();
