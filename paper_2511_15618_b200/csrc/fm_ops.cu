@@ -6,7 +6,9 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <algorithm>
 #include <atomic>
+#include <numeric>
 
 #include "fm_logprobs.cuh"
 #include "fm_pages.cuh"
@@ -129,15 +131,24 @@ int score_rows(const lp::Args& a, cudaStream_t stream) {
   return launched();
 }
 
-// Rows that share keys (nodes x heads of a group): up to 16 take the warp-level form, more the tensor cores' tiles of 256.
-inline bool few_rows(int max_nodes, int group) { return (int64_t)max_nodes * group <= 16; }
+// The form of a pass, by what the caller says of its sizes.  Rows that share keys (nodes x heads of a group): up to 16 take tiles of
+// 16 rows, warp-level products (a batch of 64, one node, 8 kv-heads of 128, 4000 positions: 195 us).  More rows would each have
+// the keys brought again, from L2 at best, so they take tensor-core tiles of 256 - but those start and end slower, and a tile
+// of 256 is one CTA's: passes too small to fill the SMs take the small tiles too.  Measured where a CTA has so many chunks
+// (OVER more a tile), small | large tiles: 2 tiles of 16, 12 chunks 23 | 41 us, 51 chunks 55 | 55, 112 chunks 97 | 78;
+// 4 to 16 tiles, 7 chunks 21 | 35 us, 15 chunks 25 | 51 and 23 | 23, 22 chunks 31 | 35 and 37 | 33, 36 chunks 41 | 38.
+inline bool few_rows(const tr::Args& a, int head_dim) {
+  const int64_t rows = (int64_t)a.max_nodes * a.G, tiles = (rows + 15) / 16;
+  if (tiles == 1) return true;
+  const int chunk = head_dim == 64 ? tr::Rows16<64>::C : tr::Rows16<128>::C;
+  const int64_t seen = a.window > 0 ? std::min<int64_t>(a.max_len, (int64_t)a.n_prefix + a.window) : a.max_len;
+  const int64_t chunks = (seen + chunk - 1) / chunk + (a.max_nodes + chunk - 1) / chunk + tr::OVER;
+  return a.batch * a.Hkv * tiles * chunks <= (tiles == 2 ? 64 : 24) * tr::SMS;
+}
 using tr::DESC_BYTES;
 static_assert(DESC_BYTES >= tr::SMS * sizeof(int4), "");
 static_assert(tr::Rows16<64>::C == 128 && tr::Rows256<64>::C == 128 && tr::Rows256<128>::C == 128 && tr::Rows16<128>::C == 64, "make_maps");
 static_assert(tr::Rows16<128>::FIXED + tr::plan_bytes(FM_MAX_TREES) <= 227 * 1024 && tr::Rows256<128>::FIXED + tr::plan_bytes(FM_MAX_TREES) <= 227 * 1024, "");
-inline size_t tree_bytes(bool few, int dh) {
-  return DESC_BYTES + (size_t)tr::SMS * 2 * (few ? 16 : 256) * (dh + 2) * sizeof(float);
-}
 
 typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
                                   const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
@@ -150,13 +161,13 @@ EncodeTiledFn encode_tiled_fn() {
   }();
   return fn;
 }
-// A layer's pool as (features, slots, heads, pages), boxes of 64 features and min(page, chunk) slots, 128-byte swizzle.
-// Boxes have to fill a chunk evenly and start where the swizzle does (8 rows); other page sizes, and strides that a map
-// cannot hold, are copied by threads.
-// (One page a sequence: any size from a chunk up, what lies behind the last slot reads as zeros.)
+// A layer's pool as (features, slots, heads, pages), boxes of 64 features and the most slots that divide pages and chunks evenly,
+// 128-byte swizzle.  Boxes have to start where the swizzle does (8 rows); other page sizes, and strides that a map cannot
+// hold, are copied by threads.  (One page a sequence: a chunk's slots, what lies behind the last one reads as zeros.)
 bool make_maps_of(const fm_cache& c, int layer, int max_pages, int chunk, tr::Args& a) {
   const int ps = c.page_slots;
-  if (!(max_pages == 1 && ps >= chunk) && (ps % 8 != 0 || (chunk % ps != 0 && ps % chunk != 0))) return false;
+  a.box_rows = max_pages == 1 && ps >= chunk ? chunk : std::gcd(ps, chunk);
+  if (a.box_rows % 8 != 0) return false;
   const EncodeTiledFn fn = encode_tiled_fn();
   if (fn == nullptr) return false;
   const int64_t most = (int64_t)1 << 39;
@@ -164,7 +175,7 @@ bool make_maps_of(const fm_cache& c, int layer, int max_pages, int chunk, tr::Ar
     if (s <= 0 || s >= most) return false;
   const cuuint64_t dim[4] = {(cuuint64_t)c.head_dim, (cuuint64_t)ps, (cuuint64_t)c.n_kv_heads, (cuuint64_t)c.n_pages};
   const cuuint64_t stride[3] = {(cuuint64_t)c.slot_stride * 2, (cuuint64_t)c.head_stride * 2, (cuuint64_t)c.page_stride * 2};
-  const cuuint32_t box[4] = {64, (cuuint32_t)(ps < chunk ? ps : chunk), 1, 1}, one[4] = {1, 1, 1, 1};
+  const cuuint32_t box[4] = {64, (cuuint32_t)a.box_rows, 1, 1}, one[4] = {1, 1, 1, 1};
   const CUtensorMapDataType type = c.dtype == FM_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
   for (int kv = 0; kv < 2; ++kv) {
     char* base = static_cast<char*>(kv == 0 ? c.k : c.v) + 2 * layer * c.layer_stride;
@@ -184,7 +195,7 @@ inline bool whole_for_sure(const tr::Args& a, int rows, int chunk, int ctas) {
 template <typename T, int DH>
 int tree_attention(const tr::Args& a, cudaStream_t stream) {
   cudaError_t e = cudaSuccess;
-  if (few_rows(a.max_nodes, a.G)) {
+  if (few_rows(a, DH)) {
     static std::atomic<uint64_t> asked{0};
     using CF = tr::Rows16<DH>;
     if (!allow_smem(tr::rows16_kernel<T, DH>, CF::bytes(FM_MAX_TREES), asked)) return FM_ERR_CUDA;
@@ -217,9 +228,11 @@ Div div_by(int d) {
   }
   return v;
 }
-size_t workspace_bytes(int max_nodes, int group, int head_dim) { return tree_bytes(few_rows(max_nodes, group), head_dim); }
+size_t workspace_bytes(int max_nodes, int group, int head_dim) {             // (of more than 16 rows: enough for either form)
+  return DESC_BYTES + (size_t)SMS * 2 * ((int64_t)max_nodes * group <= 16 ? 16 : 256) * (head_dim + 2) * sizeof(float);
+}
 bool make_maps(const fm_cache& c, int layer, int max_pages, Args& a) {
-  return make_maps_of(c, layer, max_pages, few_rows(a.max_nodes, a.G) && c.head_dim == 128 ? 64 : 128, a);
+  return make_maps_of(c, layer, max_pages, few_rows(a, c.head_dim) && c.head_dim == 128 ? tr::Rows16<128>::C : 128, a);
 }
 int launch(const Args& a, int dtype, int head_dim, cudaStream_t stream) {
   if (dtype == FM_BF16) return head_dim == 64 ? tree_attention<bf16, 64>(a, stream) : tree_attention<bf16, 128>(a, stream);

@@ -5,9 +5,9 @@
 // per SM whatever the lengths: the chunks of all tiles, one tile after the other, are cut into equal shares (their total is
 // known on the device alone), so ragged batches are balanced without the host.  A cut falls inside a tile at most once per CTA; the
 // parts of a cut tile go to a scratch buffer and a second small launch merges them in order.
-// Loading: a page's slots (or a chunk's, where pages are larger) of a head are one TMA box, swizzled for the multiplication; one warp
-// requests chunks ahead of the warps that multiply, through a ring of stages.  Page sizes whose boxes do not fill a chunk
-// evenly, and the nodes' rows, are copied 16 bytes a thread (cp.async) into the same layout.
+// Loading: a page's slots (or a chunk's, or as many as fit evenly into both) of a head are one TMA box, swizzled for the
+// multiplication; warps of their own request chunks ahead, through a ring of stages.  Pages that are no multiple of 8 slots, and
+// the nodes' rows, are copied 16 bytes a thread (cp.async) into the same layout (at a third of the rate).
 // Ancestors: reach[i], a bit per node, by pointer doubling over the parents (log2 of the depth rounds).
 // Values a row does not see have no effect on it: scores are replaced by -inf; values that are not finite in chunks
 // where some row does not see all keys are taken out of the product and added to the rows that do see them.
@@ -45,8 +45,8 @@ struct Args {
   float scale_log2;
   int ring;                             // 0, or: positions behind the prefix wrap around after so many slots (one page per sequence)
   int lo_off;                           // 0, or: rows are [hi | lo] bfloat16 terms, lo so many elements behind hi
-  int tma;                              // the page size suits the boxes
-  alignas(64) CUtensorMap map_k, map_v; // the layer's pool as [pages][heads][slots][head_dim], box 64 features x min(page, C) slots
+  int tma, box_rows;                    // the page size suits boxes, of so many slots
+  alignas(64) CUtensorMap map_k, map_v; // the layer's pool as [pages][heads][slots][head_dim], box 64 features x box_rows slots
 };
 
 // ---- element types
@@ -303,7 +303,7 @@ __device__ inline void fetch_ids(const Args& a, const Seq& s, const Chunk& k, in
   if (k.tree) return;
   const int* table = a.table + (int64_t)s.seq * a.max_pages;
   if (boxed(a, k)) {
-    const int rows = min(a.page_div.d, C), slot = place_of(a, k.start + lane * rows), pi = a.page_div(slot);      // (at most C / 8 = 16 boxes)
+    const int rows = a.box_rows, slot = place_of(a, k.start + lane * rows), pi = a.page_div(slot);      // (at most C / 8 = 16 boxes)
     x.id[0] = lane * rows < k.n ? __ldg(table + pi) : -1;
     x.in_page = slot - pi * a.page_div.d;
   } else {
@@ -315,7 +315,7 @@ __device__ inline void fetch_ids(const Args& a, const Seq& s, const Chunk& k, in
 template <int C>
 __device__ inline void request_boxes(const Args& a, const CUtensorMap* map, int x0, const Chunk& k, const Ids<C>& x, int first, int step, int hk, unsigned char* to,
                                      uint64_t* bar, int lane) {
-  const int rows = min(a.page_div.d, C);
+  const int rows = a.box_rows;
   const bool mine = lane * rows < k.n && lane % step == first, ok = mine && x.id[0] >= 0 && x.id[0] < a.n_pages;
   if (mine && !ok) {                                         // no page: zeros, and the caller is told
     if (a.status != nullptr) atomicMin(a.status, FM_ERR_INVALID_ARG);
@@ -980,7 +980,7 @@ __global__ void __launch_bounds__(Rows256<DH>::THREADS, 1) rows256_kernel(const 
         if (boxed(a, k)) {
           // (both halves of a box in a lane: they land on one barrier, which every lane arrives on once)
           const CUtensorMap* map = v ? &a.map_v : &a.map_k;
-          const int rows = min(a.page_div.d, C);
+          const int rows = a.box_rows;
           const bool has = lane * rows < k.n, good = has && x.id[0] >= 0 && x.id[0] < a.n_pages;
           unsigned char* to = (v ? Vs : Ks) + lane * rows * 128;
           if (has && !good) {                                // no page: zeros, and the caller is told
@@ -1434,7 +1434,7 @@ static __global__ void __launch_bounds__(128) accept_kernel(const int* tokens, c
 constexpr size_t DESC_BYTES = 8192;      // in front of a workspace's parts: what the merge has to do, of the CTAs
 // Launches, for the entry points and for the context's own passes (fm_ops.cu).
 size_t workspace_bytes(int max_nodes, int group, int head_dim);
-bool make_maps(const fm_cache& c, int layer, int max_pages, Args& a);          // a.max_nodes and a.G are set
+bool make_maps(const fm_cache& c, int layer, int max_pages, Args& a);          // the sizes in `a` are set
 int launch(const Args& a, int dtype, int head_dim, cudaStream_t stream);
 Div div_by(int d);
 

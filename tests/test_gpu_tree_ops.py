@@ -522,3 +522,16 @@ def test_scores_of_few_and_of_many_rows(rows, vocab):
     x = torch.randn((rows, vocab), device="cuda").to(BF)
     t = torch.randint(vocab, (rows,), device="cuda", dtype=torch.int32)
     check_scores(x, t, 6, logprobs(x, t, top=6))
+
+
+@pytest.mark.parametrize("page", [8, 24, 40, 48, 72, 96, 160, 200])
+@pytest.mark.parametrize("dh", [64, 128])
+def test_pages_that_chunks_do_not_divide(page, dh):
+    run_case(41, [0, 7, 8, 200, 777], [3, 1, 5, 2, 7], 4, 2, dh, page, BF)
+    run_case(42, [500, 130], [20, 3], 2, 1, dh, page, HF, window=100, prefix=30)
+
+
+@pytest.mark.parametrize("dh,nodes", [(64, 40), (128, 20), (64, 256), (128, 130)])
+def test_trees_of_several_small_tiles(dh, nodes):
+    run_case(43, [1500, 3, 260], [nodes, 1, nodes - 3], 3, 1, dh, 64, BF)
+    run_case(44, [1500], [nodes], 2, 2, dh, 16, HF, window=400, prefix=70)
