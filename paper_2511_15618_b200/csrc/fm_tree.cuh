@@ -121,8 +121,11 @@ __device__ inline Seq sequence(const Args& a, int4 v) {
   return s;
 }
 
-// ---- the cut of all chunks into shares.  A tile counts OVER chunks more than it has: what starting and ending it takes.
-constexpr int OVER = 4;
+// ---- the cut of all chunks into shares.  A tile counts OVER chunks more than it has: what starting and ending it takes.  (2, 4, 6, 8:
+// geometric means over 17 ragged and even batches of 97.5, 95.4, 94.1 and 95.3 us.)  A cut of up to NEAR chunks off the border
+// of a tile moves there; an eighth of a share in place of 3 chunks left some CTAs a quarter more than others (202 for 179 us
+// at 64 sequences of 4000 positions, 8 kv-heads of 128).
+constexpr int OVER = 6, NEAR = 3;
 struct Plan {
   const long long* base;                // [batch + 1] units in front of a sequence's
   const int* tile_base;                 // [batch + 1] tiles in front of a sequence's
@@ -149,7 +152,7 @@ __device__ inline long long boundary(const Args& a, const Plan& p, int i) {
   if (x >= p.total) return p.total;
   const int b = find(p.base, p.batch, x), units = sequence<C, ROWS>(a, p.info[b]).chunks + OVER;
   const int off = (int)((x - p.base[b]) % units);
-  const long long near = p.share >> 3;
+  const long long near = (p.share >> 3) < NEAR ? (p.share >> 3) : NEAR;
   if (off <= near + OVER) return x - off;
   if (units - off <= near) return x - off + units;
   return x;
@@ -1045,7 +1048,7 @@ __global__ void __launch_bounds__(Rows256<DH>::THREADS, 1) rows256_kernel(const 
     asm volatile("cp.async.wait_all;" ::: "memory");
   } else if (warp == 2) {
     // ---- multiplying.  Scores run two steps ahead of the products with values, inside a tile.
-    const uint32_t id_s = instr_desc<T>(C), id_o = instr_desc<T>(64) | (1u << 16);          // B of P V is MN-major
+    const uint32_t id_s = instr_desc<T>(C), id_o = instr_desc<T>(DH) | (1u << 16);          // B of P V is MN-major
     const uint64_t dq = tc::smem_desc_sw128(ptx::smem_u32(sm));
     int g = 0, it = 0, part = 0;                             // step, chunk of the ring, tile
     bool ok = true;
@@ -1076,14 +1079,13 @@ __global__ void __launch_bounds__(Rows256<DH>::THREADS, 1) rows256_kernel(const 
         if (sub == 0 && !(ok = wait(full_v + st, (i / ST) & 1) && wait(fixed + st, (i / ST) & 1))) break;
         if (!(ok = wait(p_full + slot, ((g + k) >> 1) & 1))) break;
         tc::fence_after();
-        const uint64_t dv = tc::smem_desc_sw128(ptx::smem_u32(ring + st * STAGE + TILE));
+        // (MN-major: the leading offset is that between the halves of 64 features, the stride offset that between 8 keys)
+        const uint64_t dv = tc::smem_desc_sw128(ptx::smem_u32(ring + st * STAGE + TILE)) + ((uint64_t)(C * 128 / 16 - 1) << 16);
         const uint32_t tO = tmem + CF::O_AT + slot * DH, tP = tmem + (CF::ALIAS ? slot * C : CF::P_AT + slot * C / 2);
         const bool fresh = k < 2;                            // the slot's first product of the tile
         if (ptx::elect_one()) {
 #pragma unroll
-          for (int h = 0; h < DH / 64; ++h)
-#pragma unroll
-            for (int j = 0; j < C / 16; ++j) mma_ts(tO + 64 * h, tP + 8 * j, dv + h * (C * 128 / 16) + 128 * j, id_o, (!fresh || j > 0) ? 1u : 0u);
+          for (int j = 0; j < C / 16; ++j) mma_ts(tO, tP + 8 * j, dv + 128 * j, id_o, (!fresh || j > 0) ? 1u : 0u);
           tc::commit(o_full + slot);
           if (per == 1 || sub == 1) tc::commit(free_v + st);
         }
