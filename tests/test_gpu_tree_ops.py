@@ -535,3 +535,20 @@ def test_pages_that_chunks_do_not_divide(page, dh):
 def test_trees_of_several_small_tiles(dh, nodes):
     run_case(43, [1500, 3, 260], [nodes, 1, nodes - 3], 3, 1, dh, 64, BF)
     run_case(44, [1500], [nodes], 2, 2, dh, 16, HF, window=400, prefix=70)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, BF, HF])
+@pytest.mark.parametrize("offset", [-60000.0, -8193.0, -8192.0, -700.0, 5.3, 8190.0, 8300.0, 50000.0])
+def test_scores_far_from_zero(dtype, offset):
+    """The form of the differences changes with the maximum; also where it rises past the change inside a row, and from -inf."""
+    torch.manual_seed(int(offset))
+    x = torch.randn((6, 9001), device="cuda") * 3 + offset
+    x[1] = torch.linspace(offset - 900, offset + 900, 9001, device="cuda")
+    x[2] = torch.linspace(offset + 900, offset - 900, 9001, device="cuda")
+    x[3, :8000] = float("-inf")
+    x[4, ::3] = -65504.0 if dtype is HF else -1e30
+    x[5, 4500:] += 60 if dtype is HF else 3e4
+    x = x.to(dtype)
+    tokens = dev([0, 9000, 17, 8500, 3, 4600])
+    for top in (0, 20):
+        check_scores(x, tokens, top, logprobs(x, tokens, top=top))
