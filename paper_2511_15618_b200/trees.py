@@ -1,14 +1,13 @@
 """Trees of drafts over a paged cache, and token scores: binding of the calls of include/flashmesh.h that need no context.
 
-`PagedCache` owns (or is laid over) the tensors of a pool of cache pages and forwards to the C entry points;
-`tree_accept` and `logprobs` are functions of tensors.  Everything is enqueued on torch's current stream of the tensors'
-device, allocates through torch and can be captured into a CUDA graph.  There is no CPU path.
+`PagedCache` owns (or is laid over) the tensors of a pool of cache pages and forwards to the C entry points, by way of native
+functions that check the tensors (csrc/trees_host.cpp); `tree_accept` and `logprobs` are functions of tensors.  Everything is
+enqueued on torch's current stream of the tensors' device, allocates through torch and can be captured into a CUDA graph.
+There is no CPU path.
 """
 from __future__ import annotations
 
 import ctypes as C
-import math
-import struct
 
 import torch
 
@@ -33,10 +32,6 @@ class FmPages(C.Structure):
                 ("lens", C.c_void_p), ("refs", C.c_void_p), ("status", C.c_void_p), ("work", C.c_void_p)]
 
 
-# FmNewRows and FmTreeArgs as struct.pack writes them (native sizes and alignment)
-_ROWS, _TREE = struct.Struct("PPqqq"), struct.Struct("PPPPPqqqPPPPPPiiiiiiiif0P")
-
-
 class FmNewRows(C.Structure):
     _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("layer_stride", C.c_int64), ("row_stride", C.c_int64), ("head_stride", C.c_int64)]
 
@@ -49,7 +44,7 @@ class FmTreeArgs(C.Structure):
                 ("max_len", C.c_int32), ("window", C.c_int32), ("n_prefix", C.c_int32), ("scale", C.c_float)]
 
 
-_LIB = None
+_LIB = _HOST = None
 
 
 def _lib():
@@ -76,6 +71,17 @@ def _lib():
     return _LIB
 
 
+def _host():
+    """The native functions of csrc/trees_host.cpp: checks, outputs, workspaces and the call in one."""
+    global _HOST
+    if _HOST is None:
+        _lib()                                             # (built and loaded)
+        from . import _trees
+        _trees.set_error(FmError)
+        _HOST = _trees
+    return _HOST
+
+
 def _need(ok, what):
     if not ok:
         raise FmError(-1, what)
@@ -91,19 +97,6 @@ def _ids(t, device, what):
     if t.dtype is not torch.int32 or t.device != device or not t.is_contiguous():
         raise FmError(-1, f"{what}: a contiguous int32 tensor on {device}")
     return t.data_ptr()
-
-
-# A decode loop makes a handful of these calls per pass, each of which takes the device a few microseconds: the address of
-# the current stream without the Stream object around it (2 us), argument blocks packed instead of filled field by field.
-_stream_of = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
-
-
-def _on(index, call, *args):
-    """call(*args, stream) on torch's current stream of device `index`, with the device current."""
-    if torch.cuda.current_device() == index:
-        return call(*args, _stream_of(index))
-    with torch.cuda.device(index):
-        return call(*args, _stream_of(index))
 
 
 class PagedCache:
@@ -148,12 +141,7 @@ class PagedCache:
                               self.head_dim, types[k.dtype])
         self._pages = FmPages(self.n_pages, self.page_slots, self.max_seqs, self.max_pages, _ids(table, self.device, "table"),
                               _ids(lens, self.device, "lens"), _ids(refs, self.device, "refs"), self.status.data_ptr(), self.work.data_ptr())
-        self._sizes = {}                                   # workspace bytes by (heads, max_nodes)
-        self._cache_p, self._pages_p = C.byref(self._cache), C.byref(self._pages)
-
-    def _list(self, a, b, what):
-        _need(a.dim() == 1 and a.shape == b.shape, f"{what}: two lists of the same length")
-        return _ids(a, self.device, what), _ids(b, self.device, what), a.numel()
+        self._at = C.addressof(self._cache), C.addressof(self._pages), self.device.index
 
     def check(self):
         """Waits for the device; raises FmError for the error it has recorded (of several the lowest code), and clears it."""
@@ -164,49 +152,29 @@ class PagedCache:
 
     def reset(self):
         """All pages free, all sequences empty."""
-        _check(_on(self.device.index, _lib().fm_pages_reset, self._pages_p), "fm_pages_reset")
+        with torch.cuda.device(self.device):
+            _check(_lib().fm_pages_reset(C.byref(self._pages), torch.cuda.current_stream().cuda_stream), "fm_pages_reset")
 
     def fork(self, src, dst):
         """Sequences dst become copies of src that share their pages (int32 lists on the device; negative: skipped)."""
-        s, d, n = self._list(src, dst, "fork")
-        _check(_on(self.device.index, _lib().fm_pages_fork, self._pages_p, s, d, n), "fm_pages_fork")
+        _host().fork(*self._at, src, dst)
 
     def reserve(self, seqs, grow):
         """Pages of their own for grow[i] more positions of sequence seqs[i] (a shared last page is copied)."""
-        s, g, n = self._list(seqs, grow, "reserve")
-        _check(_on(self.device.index, _lib().fm_pages_reserve, self._pages_p, self._cache_p, s, g, n), "fm_pages_reserve")
+        _host().reserve(*self._at, seqs, grow)
 
     def append(self, seqs, k_new, v_new, row_off, path=None, n_acc=None, max_rows=None):
         """Write rows of k_new, v_new [layers, rows, kv heads, head_dim] behind the sequences and advance their lengths: all rows
         row_off[i]..row_off[i+1]-1 of entry i, or those that path [n, stride] / n_acc [n] name (see `tree_accept`)."""
-        n = seqs.numel()
-        _need(seqs.dim() == 1 and row_off.shape == (n + 1,), "append: seqs [n], row_off [n + 1]")
-        _need(k_new.dim() == 4 and k_new.shape == v_new.shape and k_new.stride() == v_new.stride() and k_new.stride(3) == 1 and k_new.dtype == v_new.dtype == self.dtype and
-              k_new.device == v_new.device == self.device and (k_new.shape[0], k_new.shape[2], k_new.shape[3]) == (self.n_layers, self.n_kv_heads, self.head_dim),
-              "append: k_new and v_new [layers, rows, kv heads, head_dim] of the cache's type, with the same strides")
-        _need((path is None) == (n_acc is None), "append: path and n_acc go together")
-        stride = 0
-        if path is not None:
-            _need(path.dim() == 2 and path.shape[0] == n and n_acc.shape == (n,), "append: path [n, stride], n_acc [n]")
-            stride = path.shape[1]
-        if max_rows is None:
-            max_rows = stride if path is not None else k_new.shape[1]
-        s = k_new.stride()
-        rows = _ROWS.pack(k_new.data_ptr(), v_new.data_ptr(), s[0], s[1], s[2])
-        _check(_on(self.device.index, _lib().fm_pages_append, self._pages_p, self._cache_p, rows, _ids(seqs, self.device, "seqs"),
-                   _ids(row_off, self.device, "row_off"), _ids(path, self.device, "path") if path is not None else None, stride,
-                   _ids(n_acc, self.device, "n_acc") if path is not None else None, n, max_rows), "fm_pages_append")
+        _host().append(*self._at, seqs, k_new, v_new, row_off, path, n_acc, max_rows)
 
     def truncate(self, seqs, lens):
         """Cut sequences seqs[i] to at most lens[i] positions and give back the pages behind them (0: all)."""
-        s, l, n = self._list(seqs, lens, "truncate")
-        _check(_on(self.device.index, _lib().fm_pages_truncate, self._pages_p, s, l, n), "fm_pages_truncate")
+        _host().truncate(*self._at, seqs, lens)
 
     def compact(self):
         """Move the pages in use to the front of the pool; returns their number (int32 [1], on the device)."""
-        used = torch.empty(1, dtype=torch.int32, device=self.device)
-        _check(_on(self.device.index, _lib().fm_pages_compact, self._pages_p, self._cache_p, used.data_ptr()), "fm_pages_compact")
-        return used
+        return _host().compact(*self._at, self.table)
 
     def attention(self, layer, q, k_new, v_new, row_off, parent, seqs=None, window=0, n_prefix=0, scale=None, max_nodes=None, max_len=None,
                   want_lse=False, out=None):
@@ -215,72 +183,16 @@ class PagedCache:
         q [rows, heads, head_dim], k_new, v_new [rows, kv heads, head_dim] (rows may lie apart); row_off [n + 1]; parent [rows]: an earlier
         node of the tree, counted from its first row, or -1.  seqs [n]: the trees' sequences (None: 0 .. n-1).  max_nodes, max_len:
         bounds on a tree's nodes and a sequence's positions (default: what there is room for).  Returns out, or (out, lse)."""
-        rows, heads, dh = q.shape if q.dim() == 3 else (0, 0, 0)
-        n = row_off.numel() - 1
-        _need(rows > 0 and q.stride(2) == 1 and q.stride(1) == dh == self.head_dim and q.dtype == self.dtype and q.device == self.device,
-              "attention: q [rows, heads, head_dim] of the cache's type")
-        _need(k_new.shape == v_new.shape == (rows, self.n_kv_heads, dh) and k_new.stride() == v_new.stride() and k_new.stride(2) == 1 and
-              k_new.stride(1) == dh and k_new.dtype == v_new.dtype == self.dtype and k_new.device == v_new.device == self.device,
-              "attention: k_new and v_new [rows, kv heads, head_dim] of the cache's type, with the same strides")
-        _need(n >= 1 and parent.shape == (rows,) and (seqs is None and n <= self.max_seqs or seqs is not None and seqs.shape == (n,)),
-              "attention: row_off [n + 1], parent [rows], seqs [n]")
-        if out is None:
-            out = q.new_empty((rows, heads, dh))
-        else:
-            _need(out.shape == q.shape and out.dtype == q.dtype and out.device == self.device and out.stride(2) == 1 and out.stride(1) == dh, "attention: out like q")
-        lse = torch.empty((rows, heads), dtype=torch.float32, device=self.device) if want_lse else None
-        if max_nodes is None:
-            max_nodes = min(rows, FM_MAX_TREE_NODES)
-        # (a single row has no distance to the next one that matters)
-        q_row, new_row, out_row = (q.stride(0), k_new.stride(0), out.stride(0)) if rows > 1 else (heads * dh, self.n_kv_heads * dh, heads * dh)
-        p = self._pages
-        try:
-            a = _TREE.pack(q.data_ptr(), k_new.data_ptr(), v_new.data_ptr(), out.data_ptr(), lse.data_ptr() if want_lse else 0, q_row, new_row, out_row,
-                           p.table, p.lens, _ids(seqs, self.device, "seqs") if seqs is not None else 0, _ids(row_off, self.device, "row_off"),
-                           _ids(parent, self.device, "parent"), p.status, self.max_pages, self.max_seqs, n, heads, max_nodes,
-                           self.max_pages * self.page_slots if max_len is None else max_len, window, n_prefix, 1.0 / math.sqrt(dh) if scale is None else scale)
-        except (struct.error, OverflowError):
-            raise FmError(-1, "attention: a number out of range") from None
-        lib, size = _lib(), self._sizes.get((heads, max_nodes))
-        if size is None:
-            size = lib.fm_tree_attention_bytes(self._cache_p, a)     # (0 where the call itself will refuse)
-            if size:
-                self._sizes[heads, max_nodes] = size
-        work = torch.empty(size or 1, dtype=torch.uint8, device=self.device)
-        _check(_on(self.device.index, lib.fm_tree_attention, self._cache_p, layer, a, work.data_ptr(), size), "fm_tree_attention")
-        return (out, lse) if want_lse else out
+        return _host().attention(*self._at, layer, q, k_new, v_new, row_off, parent, seqs, window, n_prefix, scale, max_nodes, max_len, want_lse, out)
 
 
 def tree_accept(tokens, parent, row_off, predicted, max_nodes=None):
     """The longest path of every tree that the predictions confirm: (path [n, max_nodes] node indices, then -1; n_acc [n];
     next_token [n]).  tokens, parent, predicted [rows], row_off [n + 1]: int32 on the device."""
-    device, n, rows = tokens.device, row_off.numel() - 1, tokens.numel()
-    _need(tokens.is_cuda and tokens.dim() == 1 and parent.shape == predicted.shape == tokens.shape and n >= 1, "tree_accept: tokens, parent, predicted [rows]; row_off [n + 1]")
-    stride = min(max(rows, 1), FM_MAX_TREE_NODES) if max_nodes is None else max_nodes
-    path, n_acc, nxt = tokens.new_empty((n, max(stride, 0))), tokens.new_empty(n), tokens.new_empty(n)
-    _check(_on(device.index, _lib().fm_tree_accept, _ids(tokens, device, "tokens"), _ids(parent, device, "parent"), _ids(row_off, device, "row_off"),
-               _ids(predicted, device, "predicted"), n, path.data_ptr(), stride, n_acc.data_ptr(), nxt.data_ptr()), "fm_tree_accept")
-    return path, n_acc, nxt
-
-
-_SCORED = {torch.float32: FM_FP32, torch.bfloat16: FM_BF16, torch.float16: FM_FP16}
+    return _host().accept(tokens, parent, row_off, predicted, max_nodes)
 
 
 def logprobs(logits, tokens=None, top=0):
     """Scores of logits rows [rows, vocab] (float32, bfloat16 or float16; rows may lie apart): (logprob [rows], entropy [rows], rank
     [rows], top_ids [rows, top], top_logprobs [rows, top]).  tokens: int32 [rows], or None (logprob -inf, rank -1)."""
-    kind = _SCORED.get(logits.dtype)
-    _need(kind is not None and logits.dim() == 2 and logits.is_cuda and logits.shape[1] >= 1 and (logits.stride(1) == 1 or logits.shape[1] == 1),
-          "logprobs: logits [rows, vocab] in float32, bfloat16 or float16 on a CUDA device")
-    rows, vocab = logits.shape
-    device = logits.device
-    _need(0 <= top <= vocab and (tokens is None or tokens.shape == (rows,)), "logprobs: tokens [rows], top")
-    lp = torch.empty(rows, dtype=torch.float32, device=device)
-    ent, rank = torch.empty_like(lp), torch.empty_like(lp, dtype=torch.int32)
-    tops = lp.new_empty((rows, top))
-    ids = torch.empty_like(tops, dtype=torch.int32)
-    if rows > 0:
-        _check(_on(device.index, _lib().fm_logprobs, logits.data_ptr(), kind, rows, vocab, logits.stride(0) if rows > 1 else vocab,
-                   _ids(tokens, device, "tokens") if tokens is not None else None, lp.data_ptr(), ent.data_ptr(), rank.data_ptr(), top, ids.data_ptr(),
-                   tops.data_ptr()), "fm_logprobs")
-    return lp, ent, rank, ids, tops
+    return _host().logprobs(logits, tokens, top)

@@ -43,10 +43,32 @@ def args(**kw):
     return bytes(a)
 
 
-def test_packed_argument_blocks():
-    """The formats with which the binding packs them are those of the structures."""
-    n = list(range(1, 24))
-    assert T._TREE.pack(*n) == bytes(T.FmTreeArgs(*n)) and T._ROWS.pack(*n[:5]) == bytes(T.FmNewRows(*n[:5]))
+def refused(call, *args, **kw):
+    with pytest.raises(T.FmError) as e:
+        call(*args, **kw)
+    return e.value.code == INVALID
+
+
+def test_tensors_without_a_device_are_refused(lib):
+    """The functions for torch tensors: what is no tensor, of another type or shape, or on the host."""
+    torch = pytest.importorskip("torch")
+    x, i = torch.zeros(3, 5), torch.zeros(3, dtype=torch.int32)
+    for logits in (x, x[0], x.double(), x[:, :0], None, 3):
+        assert refused(T.logprobs, logits)
+    assert refused(T.tree_accept, i, i, i, i) and refused(T.tree_accept, i, None, i, i) and refused(T.tree_accept, i[None], i, i, i)
+    host = T._host()
+    c, p = cache(), pages()
+    at = C.addressof(c), C.addressof(p), 0
+    q, kv = torch.zeros(3, 4, 64, dtype=torch.bfloat16), torch.zeros(3, 2, 64, dtype=torch.bfloat16)
+    good = [0, q, kv, kv, i[:2], i, None, 0, 0, None, None, None, False, None]
+    for k, bad in ((0, None), (0, 1 << 40), (1, None), (1, q[0]), (1, q.float()), (2, q), (3, None), (4, i[:0]), (7, 2.5), (9, "x"), (13, x), (1, q)):
+        a = list(good)
+        a[k] = bad
+        assert refused(host.attention, *at, *a), (k, bad)
+    assert refused(host.attention, *at) and refused(host.attention, 0, *at[1:], *good)
+    rows = torch.zeros(2, 3, 2, 64, dtype=torch.bfloat16)
+    for a in ([i, rows, rows, i], [i[:2], rows, rows, i, None, i], [i[:2], rows[0], rows, i], [i[:2], rows, rows, i]):
+        assert refused(host.append, *at, *(a + [None] * (7 - len(a))))
 
 
 def test_work_sizes(lib):
