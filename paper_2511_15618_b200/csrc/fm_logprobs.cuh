@@ -298,6 +298,8 @@ template <typename T, int R>
 __global__ void __launch_bounds__(32 * SHORT_WARPS) short_kernel(const Args a) {
   constexpr int N = Vec<T>::N;
   __shared__ uint64_t s_cand[SHORT_WARPS][SHORT_CAP];
+  ptx::grid_dep_wait();
+  ptx::grid_dep_launch();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, row = blockIdx.x * SHORT_WARPS + warp;
   if (row >= a.rows) return;
   const T* x = static_cast<const T*>(a.x) + (int64_t)row * a.stride;
@@ -401,6 +403,8 @@ __global__ void __launch_bounds__(THREADS) long_kernel(const Args a) {
   __shared__ Sums s_sum[NW];
   __shared__ int s_rank[NW];
   __shared__ int s_count, s_keys;
+  ptx::grid_dep_wait();
+  ptx::grid_dep_launch();
   const int row = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const T* x = static_cast<const T*>(a.x) + (int64_t)row * a.stride;
   const Cut<T> cut(x, a.vocab);

@@ -23,19 +23,20 @@ inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 
 inline cudaStream_t as_stream(void* s) { return reinterpret_cast<cudaStream_t>(s); }
 inline int launched() { return cudaGetLastError() == cudaSuccess ? FM_OK : FM_ERR_CUDA; }
 
-// second launch of a pair: its blocks may start while the first one's still run
+// The kernel's blocks may start while those of the one in front still run: all of them wait for its end first (griddepcontrol.wait)
 template <typename Kernel, typename... Args>
-cudaError_t launch_behind(Kernel kern, dim3 grid, int block, cudaStream_t stream, Args... args) {
+int launch(Kernel kern, dim3 grid, int block, int smem, cudaStream_t stream, Args... args) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = grid;
   cfg.blockDim = dim3(block);
+  cfg.dynamicSmemBytes = (size_t)smem;
   cfg.stream = stream;
   cudaLaunchAttribute at[1];
   at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   at[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = at;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, kern, args...);
+  return cudaLaunchKernelEx(&cfg, kern, args...) == cudaSuccess ? FM_OK : FM_ERR_CUDA;
 }
 
 // the kernel may use that much shared memory on the current device (asked once per device)
@@ -105,8 +106,7 @@ int check_tree(const fm_cache* c, const fm_tree_args* t) {
 
 template <typename T, int R>
 int score_short(const lp::Args& a, cudaStream_t stream) {
-  lp::short_kernel<T, R><<<(a.rows + lp::SHORT_WARPS - 1) / lp::SHORT_WARPS, 32 * lp::SHORT_WARPS, 0, stream>>>(a);
-  return launched();
+  return launch(lp::short_kernel<T, R>, dim3((a.rows + lp::SHORT_WARPS - 1) / lp::SHORT_WARPS), 32 * lp::SHORT_WARPS, 0, stream, a);
 }
 
 // Rows whose vectors fit into a warp's registers (64 values a lane) take a warp, longer ones a block: of 256 threads, or of 512
@@ -121,14 +121,10 @@ int score_rows(const lp::Args& a, cudaStream_t stream) {
     if (vectors <= MOST / 2) return score_short<T, MOST / 2>(a, stream);
     return score_short<T, MOST>(a, stream);
   }
-  if (a.rows >= 2 * 148) {
-    lp::long_kernel<T, 256, 8><<<a.rows, 256, 8 * 256 * 16, stream>>>(a);
-  } else {
-    static std::atomic<uint64_t> asked{0};
-    if (!allow_smem(lp::long_kernel<T, 512, 8>, 8 * 512 * 16, asked)) return FM_ERR_CUDA;
-    lp::long_kernel<T, 512, 8><<<a.rows, 512, 8 * 512 * 16, stream>>>(a);
-  }
-  return launched();
+  if (a.rows >= 2 * 148) return launch(lp::long_kernel<T, 256, 8>, dim3(a.rows), 256, 8 * 256 * 16, stream, a);
+  static std::atomic<uint64_t> asked{0};
+  if (!allow_smem(lp::long_kernel<T, 512, 8>, 8 * 512 * 16, asked)) return FM_ERR_CUDA;
+  return launch(lp::long_kernel<T, 512, 8>, dim3(a.rows), 512, 8 * 512 * 16, stream, a);
 }
 
 // The form of a pass, by what the caller says of its sizes.  Rows that share keys (nodes x heads of a group): up to 16 take tiles of
@@ -194,23 +190,21 @@ inline bool whole_for_sure(const tr::Args& a, int rows, int chunk, int ctas) {
 
 template <typename T, int DH>
 int tree_attention(const tr::Args& a, cudaStream_t stream) {
-  cudaError_t e = cudaSuccess;
+  int rc;
   if (few_rows(a, DH)) {
     static std::atomic<uint64_t> asked{0};
     using CF = tr::Rows16<DH>;
     if (!allow_smem(tr::rows16_kernel<T, DH>, CF::bytes(FM_MAX_TREES), asked)) return FM_ERR_CUDA;
-    tr::rows16_kernel<T, DH><<<tr::SMS, CF::THREADS, CF::bytes(a.batch), stream>>>(a);
-    if (cudaGetLastError() != cudaSuccess) return FM_ERR_CUDA;
-    if (!whole_for_sure(a, 16, CF::C, tr::SMS)) e = launch_behind(tr::merge_kernel<T, DH, 16>, dim3(tr::SMS, 4), 256, stream, a);
+    rc = ::launch(tr::rows16_kernel<T, DH>, dim3(tr::SMS), CF::THREADS, CF::bytes(a.batch), stream, a);
+    if (rc == FM_OK && !whole_for_sure(a, 16, CF::C, tr::SMS)) rc = ::launch(tr::merge_kernel<T, DH, 16>, dim3(tr::SMS, 4), 256, 0, stream, a);
   } else {
     static std::atomic<uint64_t> asked{0};
     using CF = tr::Rows256<DH>;
     if (!allow_smem(tr::rows256_kernel<T, DH>, CF::bytes(FM_MAX_TREES), asked)) return FM_ERR_CUDA;
-    tr::rows256_kernel<T, DH><<<tr::SMS, CF::THREADS, CF::bytes(a.batch), stream>>>(a);
-    if (cudaGetLastError() != cudaSuccess) return FM_ERR_CUDA;
-    if (!whole_for_sure(a, 256, CF::C, tr::SMS)) e = launch_behind(tr::merge_kernel<T, DH, 256>, dim3(tr::SMS, 16), 256, stream, a);
+    rc = ::launch(tr::rows256_kernel<T, DH>, dim3(tr::SMS), CF::THREADS, CF::bytes(a.batch), stream, a);
+    if (rc == FM_OK && !whole_for_sure(a, 256, CF::C, tr::SMS)) rc = ::launch(tr::merge_kernel<T, DH, 256>, dim3(tr::SMS, 16), 256, 0, stream, a);
   }
-  return e == cudaSuccess ? FM_OK : FM_ERR_CUDA;
+  return rc;
 }
 
 }  // namespace
@@ -261,8 +255,7 @@ int fm_pages_fork(const fm_pages* p, const int32_t* src, const int32_t* dst, int
   int rc = check_pages(p);
   if (rc == FM_OK) rc = check_list(src, dst, n);
   if (rc != FM_OK || n == 0) return rc;
-  pg::fork_kernel<<<n, 128, 0, as_stream(stream)>>>(*p, src, dst, n);
-  return launched();
+  return launch(pg::fork_kernel, dim3(n), 128, 0, as_stream(stream), *p, src, dst, (int)n);
 }
 
 int fm_pages_reserve(const fm_pages* p, const fm_cache* c, const int32_t* seqs, const int32_t* grow, int32_t n, void* stream) {
@@ -270,9 +263,8 @@ int fm_pages_reserve(const fm_pages* p, const fm_cache* c, const int32_t* seqs, 
   if (rc == FM_OK) rc = check_list(seqs, grow, n);
   if (rc == FM_OK && n > p->max_seqs) rc = FM_ERR_INVALID_ARG;       // (the jobs of the entries have a place each)
   if (rc != FM_OK || n == 0) return rc;
-  pg::reserve_plan_kernel<<<1, pg::PLAN, 0, as_stream(stream)>>>(*p, seqs, grow, n);
-  if (cudaGetLastError() != cudaSuccess) return FM_ERR_CUDA;
-  return launch_behind(pg::reserve_copy_kernel, dim3(n, 2 * c->n_layers), 256, as_stream(stream), *p, geo_of(*c)) == cudaSuccess ? FM_OK : FM_ERR_CUDA;
+  rc = launch(pg::reserve_plan_kernel, dim3(1), pg::PLAN, 0, as_stream(stream), *p, seqs, grow, (int)n);
+  return rc != FM_OK ? rc : launch(pg::reserve_copy_kernel, dim3(n, 2 * c->n_layers), 256, 0, as_stream(stream), *p, geo_of(*c));
 }
 
 int fm_pages_append(const fm_pages* p, const fm_cache* c, const fm_new_rows* rows, const int32_t* seqs, const int32_t* row_off, const int32_t* path,
@@ -288,26 +280,23 @@ int fm_pages_append(const fm_pages* p, const fm_cache* c, const fm_new_rows* row
   pg::Rows r;
   r.k = static_cast<const char*>(rows->k); r.v = static_cast<const char*>(rows->v);
   r.layer = 2 * rows->layer_stride; r.row = 2 * rows->row_stride; r.head = 2 * rows->head_stride;
-  pg::append_kernel<<<dim3(n, 2 * c->n_layers), 256, 0, as_stream(stream)>>>(*p, geo_of(*c), r, seqs, row_off, path, path_stride, n_acc, max_rows);
-  return launched();
+  return launch(pg::append_kernel, dim3(n, 2 * c->n_layers), 256, 0, as_stream(stream), *p, geo_of(*c), r, seqs, row_off, path, (int)path_stride, n_acc, (int)max_rows);
 }
 
 int fm_pages_truncate(const fm_pages* p, const int32_t* seqs, const int32_t* new_lens, int32_t n, void* stream) {
   int rc = check_pages(p);
   if (rc == FM_OK) rc = check_list(seqs, new_lens, n);
   if (rc != FM_OK || n == 0) return rc;
-  pg::truncate_kernel<<<n, 128, 0, as_stream(stream)>>>(*p, seqs, new_lens);
-  return launched();
+  return launch(pg::truncate_kernel, dim3(n), 128, 0, as_stream(stream), *p, seqs, new_lens);
 }
 
 int fm_pages_compact(const fm_pages* p, const fm_cache* c, int32_t* used, void* stream) {
-  const int rc = check_both(p, c);
+  int rc = check_both(p, c);
+  if (rc == FM_OK) rc = launch(pg::compact_plan_kernel, dim3(1), pg::PLAN, 0, as_stream(stream), *p, used);
   if (rc != FM_OK) return rc;
-  pg::compact_plan_kernel<<<1, pg::PLAN, 0, as_stream(stream)>>>(*p, used);
-  if (cudaGetLastError() != cudaSuccess) return FM_ERR_CUDA;
   // enough blocks for every SM; no more than there can be pages to move
   const int rows = 2 * c->n_layers + 1, most = p->n_pages / 2 + 1, want = (148 * 16 + rows - 1) / rows;
-  return launch_behind(pg::compact_copy_kernel, dim3(want < most ? want : most, rows), 256, as_stream(stream), *p, geo_of(*c)) == cudaSuccess ? FM_OK : FM_ERR_CUDA;
+  return launch(pg::compact_copy_kernel, dim3(want < most ? want : most, rows), 256, 0, as_stream(stream), *p, geo_of(*c));
 }
 
 size_t fm_tree_attention_bytes(const fm_cache* cache, const fm_tree_args* args) {
@@ -345,8 +334,7 @@ int fm_tree_accept(const int32_t* tokens, const int32_t* parent, const int32_t* 
   if (tokens == nullptr || parent == nullptr || row_off == nullptr || predicted == nullptr || path == nullptr || n_acc == nullptr || next_tok == nullptr)
     return FM_ERR_INVALID_ARG;
   if (batch < 1 || path_stride < 1) return FM_ERR_INVALID_ARG;
-  tr::accept_kernel<<<(batch + 3) / 4, 128, 0, as_stream(stream)>>>(tokens, parent, row_off, predicted, batch, path, path_stride, n_acc, next_tok);
-  return launched();
+  return launch(tr::accept_kernel, dim3(batch / 4 + (batch % 4 != 0)), 128, 0, as_stream(stream), tokens, parent, row_off, predicted, (int)batch, path, (int)path_stride, n_acc, next_tok);
 }
 
 int fm_logprobs(const void* logits, int32_t dtype, int32_t rows, int32_t vocab, int64_t row_stride, const int32_t* tokens, float* logprob, float* entropy,

@@ -2,7 +2,8 @@
 //
 // The bookkeeping is integers in device memory, so that a decode loop never waits for the host: fork and truncate are
 // one block per entry, reserve and compact plan in one block (prefix sums over the entries and over the free pages, in
-// id order, so the result does not depend on timing) and a second launch, under the planner's tail, moves the data.
+// id order, so the result does not depend on timing) and a second launch moves the data.  Launches of a decode loop follow one
+// another on a stream: each is already resident when the one in front ends.
 // Moving is bound by memory: 16-byte loads and stores, a block per (page or rows, layer, key or value).
 #pragma once
 #include "fm_common.cuh"
@@ -56,6 +57,8 @@ __device__ inline int entry_state(const int* ids, int e, int limit) {
 
 // ---- fork: a block per entry.  No source of the call is a destination of it, so tables read here are not written here.
 __global__ void fork_kernel(const fm_pages p, const int* src, const int* dst, int n) {
+  ptx::grid_dep_wait();
+  ptx::grid_dep_launch();
   const int e = blockIdx.x, s = src[e], d = dst[e];
   if (s < 0 || d < 0) return;
   int bad = s >= p.max_seqs || d >= p.max_seqs;
@@ -82,6 +85,8 @@ __global__ void fork_kernel(const fm_pages p, const int* src, const int* dst, in
 
 // ---- truncate: a block per entry
 __global__ void truncate_kernel(const fm_pages p, const int* seqs, const int* new_lens) {
+  ptx::grid_dep_wait();
+  ptx::grid_dep_launch();
   const int e = blockIdx.x, state = entry_state(seqs, e, p.max_seqs);
   if (state != 0) {
     if (state == 2 && threadIdx.x == 0) fail(p, FM_ERR_INVALID_ARG);
@@ -123,9 +128,10 @@ __device__ inline int block_scan(int v, int* sh, int& total) {
 
 // ---- reserve, planning: one block
 __global__ void __launch_bounds__(PLAN) reserve_plan_kernel(const fm_pages p, const int* seqs, const int* grow, int n) {
+  ptx::grid_dep_wait();
+  ptx::grid_dep_launch();
   __shared__ int s_seq[FM_MAX_SEQS], s_held[FM_MAX_SEQS];    // sequence or -1; partly filled last page that is to grow, or -1
   __shared__ int sh[32];
-  ptx::grid_dep_launch();
   int* list = p.work;                                        // free ids, lowest first
   int* jobs = p.work + jobs_at(p);
   for (int e = threadIdx.x; e < n; e += PLAN) s_seq[e] = seqs[e];
@@ -259,6 +265,7 @@ __device__ inline void copy_page(const Geo& g, char* base, int from, int to, int
 // ---- reserve, copies of shared pages: grid (entries, layers * 2)
 __global__ void __launch_bounds__(256) reserve_copy_kernel(const fm_pages p, const Geo g) {
   ptx::grid_dep_wait();
+  ptx::grid_dep_launch();
   const int* job = p.work + jobs_at(p) + 3 * blockIdx.x;
   const int old = __ldcg(job);
   if (old < 0) return;
@@ -273,6 +280,8 @@ struct Rows {
 };
 __global__ void __launch_bounds__(256) append_kernel(const fm_pages p, const Geo g, const Rows rows, const int* seqs, const int* row_off,
                                                      const int* path, int path_stride, const int* n_acc, int max_rows) {
+  ptx::grid_dep_wait();
+  ptx::grid_dep_launch();
   const int e = blockIdx.x, state = entry_state(seqs, e, p.max_seqs);
   if (state != 0) {
     if (state == 2 && threadIdx.x == 0 && blockIdx.y == 0) fail(p, FM_ERR_INVALID_ARG);
@@ -315,8 +324,9 @@ __global__ void __launch_bounds__(256) append_kernel(const fm_pages p, const Geo
 
 // ---- compact, planning: one block.  Sources all lie at or behind `used`, destinations in front of it: no page is both.
 __global__ void __launch_bounds__(PLAN) compact_plan_kernel(const fm_pages p, int* used) {
-  __shared__ int sh[32];
+  ptx::grid_dep_wait();
   ptx::grid_dep_launch();
+  __shared__ int sh[32];
   int count = 0, n_used;
   for (int64_t i = threadIdx.x; i < p.n_pages; i += PLAN) count += p.refs[i] > 0;
   block_scan(count, sh, n_used);
@@ -357,6 +367,7 @@ __global__ void __launch_bounds__(PLAN) compact_plan_kernel(const fm_pages p, in
 // grid (blocks, layers * 2 + 1): the last row of blocks rewrites the tables
 __global__ void __launch_bounds__(256) compact_copy_kernel(const fm_pages p, const Geo g) {
   ptx::grid_dep_wait();
+  ptx::grid_dep_launch();
   const int n = __ldcg(p.work + word_at(p));
   const int *list = p.work, *goes = p.work + p.n_pages;
   if ((int)blockIdx.y == 2 * g.layers) {

@@ -307,11 +307,11 @@ __device__ inline void fetch_ids(const Args& a, const Seq& s, const Chunk& k, in
   const int* table = a.table + (int64_t)s.seq * a.max_pages;
   if (boxed(a, k)) {
     const int rows = a.box_rows, slot = place_of(a, k.start + lane * rows), pi = a.page_div(slot);      // (at most C / 8 = 16 boxes)
-    x.id[0] = lane * rows < k.n ? __ldg(table + pi) : -1;
+    x.id[0] = lane * rows < k.n ? table[pi] : -1;
     x.in_page = slot - pi * a.page_div.d;
   } else {
 #pragma unroll
-    for (int j = 0; j < C / 32; ++j) x.id[j] = 32 * j + lane < k.n ? __ldg(table + a.page_div(place_of(a, k.start + 32 * j + lane))) : -1;
+    for (int j = 0; j < C / 32; ++j) x.id[j] = 32 * j + lane < k.n ? table[a.page_div(place_of(a, k.start + 32 * j + lane))] : -1;
   }
 }
 // boxes first, first + step, ... of 64 features from `x0` to `to` (rows of 128 bytes); every lane arrives on the barrier once
@@ -501,6 +501,7 @@ __global__ void __launch_bounds__(Rows16<DH>::THREADS, 1) rows16_kernel(const __
   int* s_tile_base = reinterpret_cast<int*>(&tree + 1);
   __shared__ int s_fail;
   const int warp = (int)ptx::uniform(threadIdx.x >> 5), lane = threadIdx.x & 31, g = lane >> 2, t4 = lane & 3;
+  ptx::grid_dep_wait();
   ptx::grid_dep_launch();
   if (threadIdx.x == 0) {
     s_fail = 0;
@@ -936,6 +937,7 @@ __global__ void __launch_bounds__(Rows256<DH>::THREADS, 1) rows256_kernel(const 
   int* s_tile_base = reinterpret_cast<int*>(&tree + 1);
   __shared__ int s_fail, s_bad;
   const int warp = (int)ptx::uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
+  ptx::grid_dep_wait();
   ptx::grid_dep_launch();
   if (threadIdx.x == 0) {
     s_fail = s_bad = 0;
@@ -1320,7 +1322,7 @@ __global__ void __launch_bounds__(256) merge_kernel(const __grid_constant__ Args
   constexpr int CL = DH / 32, GS = ROWS * (DH + 2);
   __shared__ float s_o[8][DH];
   __shared__ float2 s_ml[8];
-  ptx::grid_dep_wait();
+  ptx::grid_dep_wait();                                      // (dependents start at its end: blocks of the next pass beside these cost 5 us)
   const int4 d = __ldcg(a.desc + blockIdx.x);
   if (d.w < 2) return;
   const int r0 = a.row_off[d.x], n = min(a.row_off[d.x + 1] - r0, a.max_nodes), rows = min(ROWS, n * a.G - d.z * ROWS);
@@ -1424,6 +1426,8 @@ __device__ inline int walk_path(const int* tokens, const int* parent, const int*
 }
 static __global__ void __launch_bounds__(128) accept_kernel(const int* tokens, const int* parent, const int* row_off, const int* predicted, int batch,
                                                      int* path, int path_stride, int* n_acc, int* next_tok) {
+  ptx::grid_dep_wait();
+  ptx::grid_dep_launch();
   const int b = blockIdx.x * 4 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
   if (b >= batch) return;
   const int r0 = row_off[b], n = r0 < 0 ? 0 : min(row_off[b + 1] - r0, path_stride);

@@ -552,3 +552,58 @@ def test_scores_far_from_zero(dtype, offset):
     tokens = dev([0, 9000, 17, 8500, 3, 4600])
     for top in (0, 20):
         check_scores(x, tokens, top, logprobs(x, tokens, top=top))
+
+
+@pytest.mark.parametrize("captured", [False, True])
+def test_calls_that_follow_one_another_see_what_the_last_one_wrote(captured):
+    """Launches are resident before the one in front ends; lengths, tables, references and rows still arrive.  Twelve positions, one or two a
+    round, through acceptance, reservation, append, attention, fork and truncation, against the same rounds one at a time."""
+    def rounds(c, wait):
+        torch.manual_seed(5)
+        i32 = dict(dtype=torch.int32, device="cuda")
+        seqs, other, off = torch.arange(6, **i32), torch.arange(6, 12, **i32), dev(np.arange(7) * 4)
+        parent, tokens, pred = dev([-1, 0, 1, 2] * 6), dev([1, 2, 3, 4] * 6), dev([2, 3, 4, 5] * 6)
+        stop = torch.zeros(6, **i32)
+        rows = [[torch.randn((n, 24, 2, 64), device="cuda").to(BF) for n in (3, 3, 1)] for _ in range(12)]
+        q = [torch.randn((24, 4, 64), device="cuda").to(BF) for _ in range(12)]
+
+        def go():
+            out = []
+            for (k, v, _), x in zip(rows, q):
+                path, n, nxt = tree_accept(tokens, parent, off, pred, max_nodes=4); wait()
+                c.reserve(seqs, n); wait()
+                c.append(seqs, k, v, off, path, n); wait()
+                for layer in range(3):
+                    out += c.attention(layer, x, k[layer], v[layer], off, parent, seqs=seqs, max_nodes=4, want_lse=True); wait()
+                c.fork(seqs, other); wait()
+                out += c.attention(1, x, k[1], v[1], off, parent, seqs=other, max_nodes=4, want_lse=True); wait()
+                out += logprobs(out[-2].flatten(1), tokens, top=3); wait()
+                out += [nxt, c.lens.clone(), c.table.clone(), c.refs.clone(), c.compact()]; wait()
+                c.truncate(other, stop); wait()
+            return out
+        return go
+
+    def pool():
+        c = PagedCache(3, 90, 4, 2, 64, 12, 14)
+        c.reset()
+        return c
+    a, b = pool(), pool()
+    want = rounds(a, torch.cuda.synchronize)()
+    go = rounds(b, lambda: None)
+    if captured:
+        side = torch.cuda.Stream()
+        g = torch.cuda.CUDAGraph()
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            with torch.cuda.graph(g, stream=side):
+                got = go()
+            for _ in range(3):
+                b.reset()
+                g.replay()
+    else:
+        go()
+        b.reset()
+        got = go()
+    torch.cuda.synchronize()
+    a.check(), b.check()
+    assert all(torch.equal(x, y) for x, y in zip(want, got)) and torch.equal(a.lens, b.lens) and int(b.lens[0]) == 48
