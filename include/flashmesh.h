@@ -433,6 +433,10 @@ int fm_device_status(fm_ctx* ctx);
  *   - What only the device sees (an id out of range, an exhausted pool) never leads to an access out
  *     of bounds: the entry concerned is left as it was and, where a call has a status word, the error
  *     is recorded there (DEV int32, 0 = none; of several the lowest code stays; the caller clears it).
+ *     Row offsets (row_off) are taken at their word, like the sizes of buffers: they ascend and stay
+ *     inside the rows that the caller has.
+ *   - A kernel enqueued behind these calls with programmatic stream serialization (its blocks may start
+ *     before they end) has to wait for them with griddepcontrol.wait before it touches their buffers.
  *   - A call may be enqueued while earlier ones on the same buffers run on the same stream.  Calls on
  *     the same fm_pages, or with the same workspace, from two streams (or two graphs that may run at
  *     the same time) have to be ordered by the caller.
@@ -450,7 +454,8 @@ int fm_device_status(fm_ctx* ctx);
 
 /* A pool of cache pages: element i of the key of position `slot` of page `page`, head h, layer l is
  * k[l*layer_stride + page*page_stride + h*head_stride + slot*slot_stride + i]; values alike.  Strides
- * in elements, multiples of 8; k and v 16-byte aligned.  The same page ids serve every layer. */
+ * in elements, multiples of 8; k and v 16-byte aligned.  The same page ids serve every layer.  Errors of all calls: INVALID_ARG (size,
+ * stride, alignment), UNSUPPORTED (dtype), CAPACITY (more than 32766 layers, or than 2^30 pieces of 16 bytes in a page of a layer). */
 typedef struct fm_cache {
   void* k; void* v;                 /* DEV                                                          */
   int64_t layer_stride, page_stride, head_stride, slot_stride;
@@ -496,7 +501,7 @@ int fm_pages_reserve(const fm_pages* pages, const fm_cache* cache, const int32_t
  * of row r, layer l: k_new[l*new_layer_stride + r*new_row_stride + h*new_head_stride + j]; strides multiples of 8, 16-byte aligned).
  * path == NULL: all its rows, in order.  Otherwise rows path[i*path_stride + 0 .. n_acc[i]-1],
  * counted from row_off[i] (an accepted path of a tree).  max_rows: bound on the rows one sequence
- * appends (HOST).  An entry whose pages are not all there, or are shared (no fm_pages_reserve), with a
+ * appends (HOST; beyond 2^30 pieces of 16 bytes in a layer it is lowered to that).  An entry whose pages are not all there, or are shared (no fm_pages_reserve), with a
  * row outside its own or more rows than max_rows is skipped: BAD_STATE or INVALID_ARG in the status
  * word; its length stays.  Ids as in fm_pages_reserve. */
 typedef struct fm_new_rows {

@@ -18,6 +18,7 @@ namespace {
 
 constexpr int64_t MOST_SLOTS = 1 << 30;      // positions a table can hold
 constexpr int MOST_GRID = 65535;
+constexpr int MOST_PIECES = 1 << 30;         // 16-byte pieces of a page, or of the rows that an entry appends: counted in 32 bits
 
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 inline cudaStream_t as_stream(void* s) { return reinterpret_cast<cudaStream_t>(s); }
@@ -64,6 +65,7 @@ int check_cache(const fm_cache* c) {
   if (c->head_dim < 8 || c->head_dim % 8 != 0) return FM_ERR_INVALID_ARG;
   if (c->dtype != FM_BF16 && c->dtype != FM_FP16) return FM_ERR_UNSUPPORTED;
   if (c->n_layers > MOST_GRID / 2 - 1) return FM_ERR_CAPACITY;
+  if ((int64_t)c->page_slots * c->n_kv_heads * (c->head_dim / 8) > MOST_PIECES) return FM_ERR_CAPACITY;
   return FM_OK;
 }
 
@@ -280,7 +282,8 @@ int fm_pages_append(const fm_pages* p, const fm_cache* c, const fm_new_rows* row
   pg::Rows r;
   r.k = static_cast<const char*>(rows->k); r.v = static_cast<const char*>(rows->v);
   r.layer = 2 * rows->layer_stride; r.row = 2 * rows->row_stride; r.head = 2 * rows->head_stride;
-  return launch(pg::append_kernel, dim3(n, 2 * c->n_layers), 256, 0, as_stream(stream), *p, geo_of(*c), r, seqs, row_off, path, (int)path_stride, n_acc, (int)max_rows);
+  return launch(pg::append_kernel, dim3(n, 2 * c->n_layers), 256, 0, as_stream(stream), *p, geo_of(*c), r, seqs, row_off, path, (int)path_stride, n_acc,
+                std::min<int>(max_rows, MOST_PIECES / (c->n_kv_heads * (c->head_dim / 8))));
 }
 
 int fm_pages_truncate(const fm_pages* p, const int32_t* seqs, const int32_t* new_lens, int32_t n, void* stream) {

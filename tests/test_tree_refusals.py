@@ -217,3 +217,9 @@ def test_pages_of_lists():
     assert p.tables == [[2], [0, 1], [0, 3]] and data[(0, 0)][3, 0, 0, 0] == 72.0
     p.truncate([1, 0], [0, 0])
     assert p.refs() == [1, 0, 0, 1, 0] and p.compact() == 2 and p.tables[2] == [0, 1] and data[(0, 0)][1, 0, 0, 0] == 72.0
+
+
+def test_pages_too_large_to_count(lib):
+    p, c = pages(page_slots=1 << 27, max_pages=1), cache(page_slots=1 << 27, n_kv_heads=2, head_dim=64)
+    assert lib.fm_pages_compact(p, c, None, None) == CAPACITY                # 2^27 slots x 2 heads x 8 pieces
+    assert lib.fm_tree_attention_bytes(c, args(max_pages=1)) == 0
