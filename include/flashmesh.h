@@ -310,7 +310,7 @@ int fm_accept(fm_ctx* ctx, const int32_t* force_len /*DEV*/, const int32_t* forc
  * [batch, nodes, V] or NULL; margin: DEV float32 out [batch, nodes] or NULL.  Changes no cache entry and
  * does not move L; calling it twice is legal.  Its projections run in the tiled form, as a prefill's: a chain verified as a tree
  * agrees with fm_verify to rounding, not to the bit (see the statement on lossless decoding above).
- * Errors: INVALID_ARG, BAD_STATE (before fm_prefill), CAPACITY (nodes > D+1, or more rows than a prefill chunk's faces). */
+ * Errors: INVALID_ARG, BAD_STATE (before fm_prefill), CAPACITY (nodes > D+1, batch > FM_MAX_TREES, or more rows than a prefill chunk's faces). */
 int fm_verify_tree(fm_ctx* ctx, const int32_t* tokens /*DEV*/, const int32_t* parent /*DEV*/, int32_t nodes, int32_t* predicted /*DEV*/,
                    float* logits /*DEV*/, float* margin /*DEV*/);
 

@@ -26,7 +26,7 @@ struct Tree {
   int rows_alloc;
 };
 
-// one warp per sequence, its first lane (a tree has at most 28 nodes)
+// A thread per sequence: a tree has at most 28 nodes, one after the other: each needs its parent's entries.
 static __global__ void map_kernel(Dims dm, SeqState st, Tree t, const int* parent, int batch) {
   const int b = blockIdx.x * blockDim.x + threadIdx.x;
   if (b > batch) return;

@@ -15,6 +15,10 @@
 //
 // Short rows (up to 2048 values) live in the registers of a warp; long ones take a block, the threads copying
 // 2048 or 4096 vectors ahead, each into shared memory of its own (cp.async: no barrier, nothing waits for a neighbour).
+// Bound: of 16-bit values the special-function units, an exponential each, then the latency of a row's start and end: 512 rows of
+// 128011 take 39 us, with 20 alternatives 45 (20 at the copy rate; an SM has up to four rows, 16 us of exponentials); of
+// fp32 57 us (70 % of the copy rate).  40000 rows of 1027 fp32: 33 us (76 %), with 20 alternatives 72: the sorting of each
+// row's list.  Ten rows of 1027: 8 us, a launch and two round trips to memory.
 #pragma once
 #include <cuda_fp16.h>
 

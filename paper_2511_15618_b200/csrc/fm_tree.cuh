@@ -471,6 +471,9 @@ __device__ inline void build_tree(Tree& t, const int* parent, int n, int tid, Sy
 // Eight warps multiply: four take the even chunks, four the odd ones, each a fixed slice of a chunk with its own running maximum,
 // sum and output (base 2).  At the end of a tile one of the two groups hands its states over and goes on, the other merges
 // and writes: they take turns.  Four warps load, queries and parents of the next tile included.
+// Bound: memory, once the SMs are full: 64 sequences of 4000 positions, 8 kv-heads of 128, one node: 179 us, 5.86 TB/s (89 % of a
+// copy); the same of 100 to 8000 positions in pages of 16: 103 us, 4.6 TB/s (70 %: pieces of 4 KB, parts and merges of ragged shares).
+// A pass of four nodes over 150 positions takes 8.6 us: a launch, the plan, a chunk's latency and the end of a tile.
 template <int DH>
 struct Rows16 {
   static constexpr int ROWS = 16, C = DH == 64 ? 128 : 64, NW = 4, KPW = C / NW, STAGES = 4;
@@ -831,7 +834,9 @@ __global__ void __launch_bounds__(Rows16<DH>::THREADS, 1) rows16_kernel(const __
 // one (the fixer) brings queries and takes values that are not finite out of chunks with hidden keys.  What threads write is
 // made visible to the tensor cores by a proxy fence.
 // Bound: the special-function units (1024 clocks for the exponentials of 128 rows x 128 keys, about what the products of
-// heads of 128 take), or, where a tile has few rows, memory.
+// heads of 128 take) and, between them and the products, the latency of a slot's turn: 1800 clocks a step of 128 x 128.  Eight
+// sequences of 32768 positions, 64 nodes: 8 kv-heads of 128, 4 heads a group 318 us (866 TFLOP/s, at the power limit); 4
+// kv-heads of 64, 8 heads a group 262 us (525).  Few rows: 28 nodes, 16 sequences of 9000, 16 heads of 64: 174 us, 3.4 TB/s.
 template <int DH>
 struct Rows256 {
   static constexpr int ROWS = 256, C = 128, STAGES = DH == 64 ? 4 : 2;
@@ -1316,7 +1321,7 @@ __global__ void __launch_bounds__(Rows256<DH>::THREADS, 1) rows256_kernel(const 
 }
 
 // ---- parts of the tiles that were cut, merged in order: grid (CTAs, blocks per tile); two, four or eight warps a row, by the number of
-// parts (one tile over all SMs has 148: two warps a row took 20 us for them)
+// parts (a tile has up to 148)
 template <typename T, int DH, int ROWS>
 __global__ void __launch_bounds__(256) merge_kernel(const __grid_constant__ Args a) {
   constexpr int CL = DH / 32, GS = ROWS * (DH + 2);
