@@ -160,12 +160,13 @@ EncodeTiledFn encode_tiled_fn() {
   return fn;
 }
 // A layer's pool as (features, slots, heads, pages), boxes of 64 features and the most slots that divide pages and chunks evenly,
-// 128-byte swizzle.  Boxes have to start where the swizzle does (8 rows); other page sizes, and strides that a map cannot
-// hold, are copied by threads.  (One page a sequence: a chunk's slots, what lies behind the last one reads as zeros.)
+// 128-byte swizzle (a function of the address: a box may start at any row of 128 bytes).  Page sizes that take more boxes than a
+// warp has lanes, and strides that a map cannot hold, are copied by threads.  (One page a sequence: a chunk's slots, what lies
+// behind the last one reads as zeros.)
 bool make_maps_of(const fm_cache& c, int layer, int max_pages, int chunk, tr::Args& a) {
   const int ps = c.page_slots;
   a.box_rows = max_pages == 1 && ps >= chunk ? chunk : std::gcd(ps, chunk);
-  if (a.box_rows % 8 != 0) return false;
+  if (a.box_rows * 32 < chunk) return false;                 // (a lane each)
   const EncodeTiledFn fn = encode_tiled_fn();
   if (fn == nullptr) return false;
   const int64_t most = (int64_t)1 << 39;

@@ -524,7 +524,7 @@ def test_scores_of_few_and_of_many_rows(rows, vocab):
     check_scores(x, t, 6, logprobs(x, t, top=6))
 
 
-@pytest.mark.parametrize("page", [8, 24, 40, 48, 72, 96, 160, 200])
+@pytest.mark.parametrize("page", [2, 4, 6, 8, 12, 20, 24, 36, 40, 48, 72, 96, 100, 160, 200])
 @pytest.mark.parametrize("dh", [64, 128])
 def test_pages_that_chunks_do_not_divide(page, dh):
     run_case(41, [0, 7, 8, 200, 777], [3, 1, 5, 2, 7], 4, 2, dh, page, BF)

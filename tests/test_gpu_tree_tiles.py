@@ -47,7 +47,7 @@ def test_lengths(length, nodes):
     T.run_case(33, [length, 77], [nodes, 2], 4, 4, 128, 24, HF)
 
 
-@pytest.mark.parametrize("page", [1, 3, 7, 8, 16, 24, 40, 100, 256])
+@pytest.mark.parametrize("page", [1, 2, 3, 4, 6, 7, 8, 12, 16, 20, 24, 36, 40, 100, 256])
 def test_page_sizes(page):
     T.run_case(34, [211, 90], [6, 11], 4, 2, 64, page, BF)
     T.run_case(34, [330, 90], [6, 11], 4, 2, 128, page, BF)
