@@ -607,3 +607,67 @@ def test_calls_that_follow_one_another_see_what_the_last_one_wrote(captured):
     torch.cuda.synchronize()
     a.check(), b.check()
     assert all(torch.equal(x, y) for x, y in zip(want, got)) and torch.equal(a.lens, b.lens) and int(b.lens[0]) == 48
+
+
+def plain_tree(c, b, n, tree, q, kn, vn, window=0, prefix=0):
+    k, v = gathered(c, 0, b, n, kn, vn)
+    return R.attention(q.double().cpu().numpy(), k, v, R.visible(tree, n, window, prefix), c.head_dim ** -0.5, UNIT[c.dtype])
+
+
+@pytest.mark.parametrize("dh", [64, 128])
+def test_one_sequence_in_several_trees_and_bounded_positions(dh):
+    rng = np.random.default_rng(51)
+    c = filled(rng, [300, 90], 2, dh, 16, BF)
+    trees = [random_tree(rng, n) for n in (5, 9, 1, 30)]
+    seqs, rows = [0, 0, 1, 0], 45
+    q, kn, vn = (torch.randn((rows, h, dh), device="cuda").to(BF) for h in (4, 2, 2))
+    off = np.concatenate([[0], np.cumsum([len(t) for t in trees])])
+    for most in (1600, 300, 137, 1, 0):
+        out, lse = c.attention(0, q, kn, vn, dev(off), dev(sum(trees, [])), seqs=dev(seqs), max_len=most, want_lse=True)
+        for i, (b, tree) in enumerate(zip(seqs, trees)):
+            at = slice(off[i], off[i + 1])
+            want, wl, to, tl = plain_tree(c, b, min([300, 90][b], most), tree, q[at], kn[at], vn[at])
+            assert (np.abs(out[at].double().cpu().numpy() - want) <= to).all()
+            live = ~np.isneginf(wl)
+            got = lse[at].double().cpu().numpy()
+            assert (np.isneginf(got) == ~live).all() and (np.abs(got[live] - wl[live]) <= tl[live]).all()
+    c.check()
+
+
+def test_the_most_trees_and_one_more():
+    n = 513
+    c = PagedCache(1, n, 16, 1, 64, n, 1)
+    c.reset()
+    seqs = torch.arange(n, dtype=torch.int32, device="cuda")
+    c.reserve(seqs, seqs % 17)
+    c.lens.copy_(seqs % 17)
+    c.k.normal_(), c.v.normal_()
+    c.check()
+    q, kn, vn = (torch.randn((n, 1, 64), device="cuda").to(BF) for _ in range(3))
+    parent = torch.full((n,), -1, dtype=torch.int32, device="cuda")
+    out = c.attention(0, q[:512], kn[:512], vn[:512], torch.arange(513, dtype=torch.int32, device="cuda"), parent[:512], max_nodes=1)
+    for b in (0, 1, 15, 16, 17, 300, 511):
+        want, _, to, _ = plain_tree(c, b, b % 17, [-1], q[b:b + 1], kn[b:b + 1], vn[b:b + 1])
+        assert (np.abs(out[b:b + 1].double().cpu().numpy() - want) <= to).all()
+    with pytest.raises(FmError) as e:
+        c.attention(0, q, kn, vn, torch.arange(n + 1, dtype=torch.int32, device="cuda"), parent, max_nodes=1)
+    assert e.value.code == -3
+
+
+def test_calls_on_a_stream_follow_what_is_enqueued_there():
+    rng = np.random.default_rng(52)
+    c = filled(rng, [200], 2, 64, 16, BF)
+    q, kn, vn = (torch.randn((3, h, 64), device="cuda").to(BF) for h in (4, 2, 2))
+    off, parent = dev([0, 3]), dev([-1, 0, 0])
+    want = c.attention(0, q, kn, vn, off, parent)
+    x, t = torch.randn((3, 5000), device="cuda"), dev([1, 2, 3])
+    scores = logprobs(x, t, top=4)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        late, late_x = torch.zeros_like(q), torch.zeros_like(x)
+        torch.cuda._sleep(20_000_000)                                     # (10 ms)
+        late.copy_(q), late_x.copy_(x)
+        got, got_scores = c.attention(0, late, kn, vn, off, parent), logprobs(late_x, t, top=4)
+    side.synchronize()
+    assert torch.equal(got, want) and all(torch.equal(a, b) for a, b in zip(got_scores, scores))
