@@ -283,7 +283,8 @@ int fm_pages_append(const fm_pages* p, const fm_cache* c, const fm_new_rows* row
   pg::Rows r;
   r.k = static_cast<const char*>(rows->k); r.v = static_cast<const char*>(rows->v);
   r.layer = 2 * rows->layer_stride; r.row = 2 * rows->row_stride; r.head = 2 * rows->head_stride;
-  return launch(pg::append_kernel, dim3(n, 2 * c->n_layers), 256, 0, as_stream(stream), *p, geo_of(*c), r, seqs, row_off, path, (int)path_stride, n_acc,
+  const int most = 2 * c->n_layers, share = (148 * 3 + n - 1) / n;           // blocks of an entry: a wave over all entries at most
+  return launch(pg::append_kernel, dim3(n, share < most ? share : most), 256, 0, as_stream(stream), *p, geo_of(*c), r, seqs, row_off, path, (int)path_stride, n_acc,
                 std::min<int>(max_rows, MOST_PIECES / (c->n_kv_heads * (c->head_dim / 8))));
 }
 

@@ -5,7 +5,7 @@
 // id order, so the result does not depend on timing) and a second launch moves the data.  Launches of a decode loop follow one
 // another on a stream: each is already resident when the one in front ends.
 // Moving is bound by memory: 16-byte loads and stores, a block per (page or rows, layer, key or value): pages of their own for 96 forks
-// of 16 sequences in 32 layers, 834 MB: 146 us, 5.7 TB/s (87 % of a copy); compaction of 1.5 GB: 285 us, 5.4 TB/s (82 %).
+// of 16 sequences in 32 layers and a row behind each, 834 MB: 131 us, 6.35 TB/s (97 % of a copy); compaction of 1.5 GB: 285 us, 5.4 TB/s (82 %).
 // Small calls are the latency of the planning chain (lengths, tables, references, free list): 5 to 7 us.
 #pragma once
 #include "fm_common.cuh"
@@ -275,7 +275,9 @@ __global__ void __launch_bounds__(256) reserve_copy_kernel(const fm_pages p, con
   copy_page(g, base, old, __ldcg(job + 1), __ldcg(job + 2));
 }
 
-// ---- append: grid (entries, layers * 2); the last block of an entry advances the length
+// ---- append: grid (entries, blocks of an entry); the last block of an entry advances the length.  A block checks the entry (a chain of six
+// dependent reads) and moves its share of the layers' keys and values, four at a time: with a block for each, forks, copies and rows of
+// 96 entries in 32 layers took 147 us in place of 131.
 struct Rows {
   const char *k, *v;
   int64_t layer, row, head;             // bytes
@@ -284,13 +286,14 @@ __global__ void __launch_bounds__(256) append_kernel(const fm_pages p, const Geo
                                                      const int* path, int path_stride, const int* n_acc, int max_rows) {
   ptx::grid_dep_wait();
   ptx::grid_dep_launch();
-  const int e = blockIdx.x, state = entry_state(seqs, e, p.max_seqs);
+  const int e = blockIdx.x, s = seqs[e], r0 = row_off[e], own = max(row_off[e + 1] - r0, 0);
+  const int n = max(path != nullptr ? n_acc[e] : own, 0);
+  const int state = entry_state(seqs, e, p.max_seqs);
   if (state != 0) {
     if (state == 2 && threadIdx.x == 0 && blockIdx.y == 0) fail(p, FM_ERR_INVALID_ARG);
     return;
   }
-  const int s = seqs[e], len = len_of(p, s), r0 = row_off[e], own = max(row_off[e + 1] - r0, 0);
-  const int n = max(path != nullptr ? n_acc[e] : own, 0);
+  const int len = len_of(p, s);
   const int* t = p.table + (int64_t)s * p.max_pages;
   // all or nothing: the pages are there and the sequence's own, the rows are its rows
   int bad = 0;
@@ -304,14 +307,28 @@ __global__ void __launch_bounds__(256) append_kernel(const fm_pages p, const Geo
   }
   const int wrong = __syncthreads_or(bad & 1), missing = __syncthreads_or(bad & 2);
   if (!wrong && !missing) {
-    char* base = ((blockIdx.y & 1) ? g.v : g.k) + (blockIdx.y >> 1) * g.layer;
-    const char* from = ((blockIdx.y & 1) ? rows.v : rows.k) + (blockIdx.y >> 1) * rows.layer;
-    const int per = g.heads * g.row16;
-    for (int i = threadIdx.x; i < n * per; i += blockDim.x) {
+    // a piece lies at the same place in every layer's keys and values; threads share the layers where there are few pieces
+    const int per = g.heads * g.row16, pieces = n * per;
+    int wide = 256;
+    while (wide > 32 && wide / 2 >= pieces) wide /= 2;
+    const int first = blockIdx.y + gridDim.y * (threadIdx.x / wide), step = gridDim.y * (256 / wide);
+    for (int i = threadIdx.x & (wide - 1); i < pieces; i += wide) {
       const int j = i / per, r = i - j * per, h = r / g.row16, c = r - h * g.row16;
       const int row = r0 + (path != nullptr ? path[(int64_t)e * path_stride + j] : j), at = len + j, pi = at / p.page_slots;
-      *reinterpret_cast<uint4*>(base + t[pi] * g.page + h * g.head + (at - pi * p.page_slots) * g.slot + 16 * c) =
-          *reinterpret_cast<const uint4*>(from + row * rows.row + h * rows.head + 16 * c);
+      const int64_t from = row * rows.row + h * rows.head + 16 * c, to = t[pi] * g.page + h * g.head + (at - pi * p.page_slots) * g.slot + 16 * c;
+      for (int l0 = first; l0 < 2 * g.layers; l0 += 4 * step) {
+        uint4 x[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const int l = l0 + u * step;
+          if (l < 2 * g.layers) x[u] = *reinterpret_cast<const uint4*>(((l & 1) ? rows.v : rows.k) + (l >> 1) * rows.layer + from);
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const int l = l0 + u * step;
+          if (l < 2 * g.layers) *reinterpret_cast<uint4*>(((l & 1) ? g.v : g.k) + (l >> 1) * g.layer + to) = x[u];
+        }
+      }
     }
   } else if (threadIdx.x == 0 && blockIdx.y == 0) {
     fail(p, wrong ? FM_ERR_INVALID_ARG : FM_ERR_BAD_STATE);
