@@ -5,7 +5,7 @@
 // id order, so the result does not depend on timing) and a second launch moves the data.  Launches of a decode loop follow one
 // another on a stream: each is already resident when the one in front ends.
 // Moving is bound by memory: 16-byte loads and stores, a block per (page or rows, layer, key or value): pages of their own for 96 forks
-// of 16 sequences in 32 layers and a row behind each, 834 MB: 131 us, 6.35 TB/s (97 % of a copy); compaction of 1.5 GB: 285 us, 5.4 TB/s (82 %).
+// of 16 sequences in 32 layers and a row behind each, 834 MB: 104 us (partly from L2); compaction of 1.5 GB: 267 us, 5.7 TB/s (87 % of a copy).
 // Small calls are the latency of the planning chain (lengths, tables, references, free list): 5 to 7 us.
 #pragma once
 #include "fm_common.cuh"
@@ -254,13 +254,25 @@ __global__ void __launch_bounds__(PLAN) reserve_plan_kernel(const fm_pages p, co
   }
 }
 
-// rows [0, slots) of every head of a page -> another page; by a block
+// rows [0, slots) of every head of a page -> another page; by a block, U pieces of a thread under way: 4 for parts of pages just
+// written or read (96 forks, 32 layers: 104 us; 8: 122, 1: 131), 8 for whole pages of a pool (1.5 GB: 267 us; 4: 277, 1: 287)
+template <int U>
 __device__ inline void copy_page(const Geo& g, char* base, int from, int to, int slots) {
-  const int per = slots * g.row16;
-  for (int i = threadIdx.x; i < g.heads * per; i += blockDim.x) {
-    const int h = i / per, r = i - h * per, s = r / g.row16, c = r - s * g.row16;
-    const int64_t at = h * g.head + s * g.slot + 16 * c;
-    *reinterpret_cast<uint4*>(base + to * g.page + at) = *reinterpret_cast<const uint4*>(base + from * g.page + at);
+  const int per = slots * g.row16, all = g.heads * per;
+  const char* src = base + from * g.page;
+  char* dst = base + to * g.page;
+  for (int i0 = threadIdx.x; i0 < all; i0 += U * blockDim.x) {
+    int64_t at[U];
+    uint4 x[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int i = i0 + u * blockDim.x, h = i / per, r = i - h * per, s = r / g.row16, c = r - s * g.row16;
+      at[u] = h * g.head + s * g.slot + 16 * c;
+      if (i < all) x[u] = *reinterpret_cast<const uint4*>(src + at[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (i0 + u * (int)blockDim.x < all) *reinterpret_cast<uint4*>(dst + at[u]) = x[u];
   }
 }
 
@@ -272,12 +284,12 @@ __global__ void __launch_bounds__(256) reserve_copy_kernel(const fm_pages p, con
   const int old = __ldcg(job);
   if (old < 0) return;
   char* base = ((blockIdx.y & 1) ? g.v : g.k) + (blockIdx.y >> 1) * g.layer;
-  copy_page(g, base, old, __ldcg(job + 1), __ldcg(job + 2));
+  copy_page<4>(g, base, old, __ldcg(job + 1), __ldcg(job + 2));
 }
 
 // ---- append: grid (entries, blocks of an entry); the last block of an entry advances the length.  A block checks the entry (a chain of six
 // dependent reads) and moves its share of the layers' keys and values, four at a time: with a block for each, forks, copies and rows of
-// 96 entries in 32 layers took 147 us in place of 131.
+// 96 entries in 32 layers took 147 us in place of 131 (before pages were copied four pieces at a time).
 struct Rows {
   const char *k, *v;
   int64_t layer, row, head;             // bytes
@@ -403,7 +415,7 @@ __global__ void __launch_bounds__(256) compact_copy_kernel(const fm_pages p, con
   }
   char* base = ((blockIdx.y & 1) ? g.v : g.k) + (blockIdx.y >> 1) * g.layer;
   for (int k = blockIdx.x; k < n; k += gridDim.x)
-    copy_page(g, base, __ldcg(list + p.n_pages - 1 - k), __ldcg(list + k), p.page_slots);
+    copy_page<8>(g, base, __ldcg(list + p.n_pages - 1 - k), __ldcg(list + k), p.page_slots);
 }
 
 }  // namespace pg
