@@ -944,7 +944,6 @@ __global__ void __launch_bounds__(Rows256<DH>::THREADS, 1) rows256_kernel(const 
   __shared__ int s_fail, s_bad;
   const int warp = (int)ptx::uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
   ptx::grid_dep_wait();
-  ptx::grid_dep_launch();
   if (threadIdx.x == 0) {
     s_fail = s_bad = 0;
     for (int i = 0; i < ST; ++i) {
@@ -967,6 +966,7 @@ __global__ void __launch_bounds__(Rows256<DH>::THREADS, 1) rows256_kernel(const 
   __syncthreads();
   tc::fence_after();
   const uint32_t tmem = ptx::uniform(*tmem_slot);
+  ptx::grid_dep_launch();                                    // (not before: a dependent's block on this SM may hold tensor memory while it waits for this grid)
   auto wait = [](uint64_t* bar, uint32_t parity) { return __all_sync(0xffffffffu, ptx::mbar_wait(bar, parity)) != 0; };
   auto two = [&] { return w.s.n * a.G - w.mt * 256 > 128; };               // more than 128 rows in the tile
 
