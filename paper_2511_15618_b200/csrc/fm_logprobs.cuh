@@ -444,8 +444,12 @@ __global__ void __launch_bounds__(THREADS) long_kernel(const Args a) {
       for (int j = 0; j < N; j += 2) mx = max3(mx, v[j], v[j + 1]);
     }
   uint32_t bound = order_of(mx);
-  if (a.top > 1) bound = sort32(bound, lane);
-  else bound = lane == 0 ? __reduce_max_sync(0xffffffffu, bound) : (__reduce_max_sync(0xffffffffu, bound), 0u);
+  if (a.top > 1) {
+    bound = sort32(bound, lane);
+  } else {
+    const uint32_t most = __reduce_max_sync(0xffffffffu, bound);             // (by all lanes at one place, then chosen)
+    bound = lane == 0 ? most : 0u;
+  }
   s_bound[warp][lane] = bound;
   for (int o = NW / 2; o > 0; o >>= 1) {
     __syncthreads();
