@@ -13,6 +13,9 @@
 // Where they do not fit (rising logits, many equal ones) the row is read again: a warp keeps the best 32 of its share
 // as a sorted list, one a lane, and takes in what exceeds its top-th.
 //
+// Rows are read by plain loads: a kernel here is resident before the launch that writes its logits has ended, so they are not
+// read-only for as long as it runs (a non-coherent load may be moved across the wait for that launch).
+//
 // Short rows (up to 2048 values) live in the registers of a warp; long ones take a block, the threads copying
 // 2048 or 4096 vectors ahead, each into shared memory of its own (cp.async: no barrier, nothing waits for a neighbour).
 // Bound: of 16-bit values the special-function units, an exponential each, then the latency of a row's start and end: 512 rows of
@@ -312,7 +315,7 @@ __global__ void __launch_bounds__(32 * SHORT_WARPS) short_kernel(const Args a) {
   uint4 raw[R];
 #pragma unroll
   for (int r = 0; r < R; ++r)
-    if (r * 32 + lane < cut.n_vec) raw[r] = __ldg(xv + r * 32 + lane);
+    if (r * 32 + lane < cut.n_vec) raw[r] = xv[r * 32 + lane];
   const int loose = cut.loose(lane, a.vocab);
   const float xl = loose >= 0 ? load1(x + loose) : -INFINITY;
   const int token = a.tokens != nullptr ? a.tokens[row] : -1;
@@ -535,7 +538,7 @@ __global__ void __launch_bounds__(THREADS) long_kernel(const Args a) {
     if (vectors <= LONG_CAP) {
       for (int i = tid; i < vectors; i += THREADS) {
         float v[N];
-        unpack(__ldg(xv + s_vec[i]), v, static_cast<const T*>(nullptr));
+        unpack(xv[s_vec[i]], v, static_cast<const T*>(nullptr));
 #pragma unroll
         for (int j = 0; j < N; ++j)
           if (v[j] >= least) collect(v[j], cut.head + s_vec[i] * N + j);
