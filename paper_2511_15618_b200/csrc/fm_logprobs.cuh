@@ -216,8 +216,8 @@ struct Cut {
   }
   // the elements outside the vectors, one a lane (fewer than 16): id, or -1
   __device__ int loose(int lane, int vocab) const {
-    const int i = lane < head ? lane : tail0 + lane - head;
-    return i < vocab && lane < head + vocab - tail0 ? i : -1;
+    const int i = lane < head ? lane : tail0 + (lane - head);
+    return lane < head + (vocab - tail0) ? i : -1;
   }
 };
 // sortable form of a value for bounds: monotonic, 0 for a NaN
@@ -292,9 +292,9 @@ __device__ inline Sums warp_sums(Sums sum, int lane) {
 template <typename T>
 __device__ __noinline__ uint64_t list_of(const T* x, int vocab, int first, int step, int top, int lane) {
   uint64_t list = 0, bar = 0;
-  for (int i0 = first; i0 < vocab; i0 += step) {
-    const int i = i0 + lane;
-    push(list, bar, i < vocab ? key_of(load1(x + i), i) : 0ull, top, lane);
+  for (unsigned i0 = first; i0 < (unsigned)vocab; i0 += step) {    // (unsigned: a step behind the last of 2^31 - 1 values)
+    const unsigned i = i0 + lane;
+    push(list, bar, i < (unsigned)vocab ? key_of(load1(x + i), (int)i) : 0ull, top, lane);
   }
   return list;
 }

@@ -108,7 +108,7 @@ int check_tree(const fm_cache* c, const fm_tree_args* t) {
 
 template <typename T, int R>
 int score_short(const lp::Args& a, cudaStream_t stream) {
-  return launch(lp::short_kernel<T, R>, dim3((a.rows + lp::SHORT_WARPS - 1) / lp::SHORT_WARPS), 32 * lp::SHORT_WARPS, 0, stream, a);
+  return launch(lp::short_kernel<T, R>, dim3(a.rows / lp::SHORT_WARPS + (a.rows % lp::SHORT_WARPS != 0)), 32 * lp::SHORT_WARPS, 0, stream, a);
 }
 
 // Rows whose vectors fit into a warp's registers (64 values a lane) take a warp, longer ones a block: of 256 threads, or of 512
