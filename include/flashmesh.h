@@ -451,6 +451,8 @@ int fm_device_status(fm_ctx* ctx);
 #define FM_MAX_TREE_NODES 256       /* nodes of one tree                                            */
 #define FM_MAX_SEQS 4096            /* sequences of one fm_pages, entries of one of its calls       */
 #define FM_MAX_TREES 512            /* trees of one fm_tree_attention                               */
+#define FM_FILL_OUT 1
+#define FM_FILL_LSE 2
 
 /* A pool of cache pages: element i of the key of position `slot` of page `page`, head h, layer l is
  * k[l*layer_stride + page*page_stride + h*head_stride + slot*slot_stride + i]; values alike.  Strides
@@ -531,8 +533,9 @@ int fm_pages_compact(const fm_pages* pages, const fm_cache* cache, int32_t* used
  * product with v); lse = log sum exp(scale q k).
  * A parent that is no earlier node and not -1 takes its node and every node below it out of use:
  * out 0, lse -inf; nobody sees them.  Values of positions and nodes that a row does not see have no
- * effect on it, whatever they hold.  Rows behind row_off[n] are left as they were.  Nodes behind max_nodes, and
- * positions behind the table or max_len, are not seen; rows of such nodes are left as they were.
+ * effect on it, whatever they hold.  Positions behind the table or max_len are not seen.  A tree of more
+ * than max_nodes nodes: CAPACITY in the status word, and the nodes behind take no part.  Their rows, and those in front of row_off[0] and
+ * behind row_off[n], are left as they were, or get what `fill` says.
  * Nothing is appended to the cache.  Errors: INVALID_ARG (null pointer, size, stride or alignment),
  * UNSUPPORTED (head_dim not 64 / 128, dtype), CAPACITY (workspace, batch > FM_MAX_TREES, max_nodes > FM_MAX_TREE_NODES). */
 typedef struct fm_tree_args {
@@ -546,9 +549,12 @@ typedef struct fm_tree_args {
   const int32_t* seqs;              /* DEV [batch] rows of table and lens, NULL: 0 .. batch-1; a negative one has no positions */
   const int32_t* row_off;           /* DEV [batch+1]                                                 */
   const int32_t* parent;            /* DEV [rows]                                                    */
-  int32_t* status;                  /* DEV [1] or NULL: TIMEOUT if a bounded wait gave up            */
+  int32_t* status;                  /* DEV [1] or NULL: CAPACITY (above), INVALID_ARG (a page id that is none, for a position
+                                     * that is seen: its key and value count as zeros), TIMEOUT if a bounded wait gave up */
   int32_t max_pages, max_seqs, batch, n_heads, max_nodes, max_len, window, n_prefix;
   float scale;                      /* above 0                                                       */
+  int32_t n_rows;                   /* rows of q, k_new, v_new, out and lse, or 0: not said          */
+  int32_t fill;                     /* rows of no tree (with n_rows): FM_FILL_OUT out 0, FM_FILL_LSE lse -inf */
 } fm_tree_args;
 size_t fm_tree_attention_bytes(const fm_cache* cache, const fm_tree_args* args);   /* workspace; 0 if the arguments are invalid */
 int fm_tree_attention(const fm_cache* cache, int32_t layer, const fm_tree_args* args, void* workspace /*DEV, 256-byte aligned*/,

@@ -100,6 +100,7 @@ int check_tree(const fm_cache* c, const fm_tree_args* t) {
   if ((t->q_row_stride | t->new_row_stride | t->out_row_stride) & 7) return FM_ERR_INVALID_ARG;
   if (t->q_row_stride < (int64_t)t->n_heads * c->head_dim || t->out_row_stride < (int64_t)t->n_heads * c->head_dim ||
       t->new_row_stride < (int64_t)c->n_kv_heads * c->head_dim) return FM_ERR_INVALID_ARG;
+  if (t->n_rows < 0 || (t->fill & ~(FM_FILL_OUT | FM_FILL_LSE)) != 0 || (t->fill != 0 && t->n_rows == 0)) return FM_ERR_INVALID_ARG;
   if (!(t->scale > 0.f) || t->scale - t->scale != 0.f) return FM_ERR_INVALID_ARG;
   if (c->head_dim != 64 && c->head_dim != 128) return FM_ERR_UNSUPPORTED;
   if (t->batch > FM_MAX_TREES || t->max_nodes > FM_MAX_TREE_NODES || (int64_t)t->max_pages * c->page_slots > MOST_SLOTS) return FM_ERR_CAPACITY;
@@ -329,6 +330,7 @@ int fm_tree_attention(const fm_cache* c, int32_t layer, const fm_tree_args* t, v
   const int64_t holds = (int64_t)t->max_pages * c->page_slots;
   a.max_len = t->max_len < holds ? t->max_len : (int)holds;
   a.window = t->window; a.n_prefix = t->n_prefix;
+  a.n_rows = t->n_rows; a.fill = t->fill;
   a.scale_log2 = t->scale * 1.4426950408889634f;
   a.tma = tr::make_maps(*c, layer, t->max_pages, a) ? 1 : 0;
   return tr::launch(a, c->dtype, c->head_dim, as_stream(stream));

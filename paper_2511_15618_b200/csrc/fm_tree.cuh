@@ -47,6 +47,7 @@ struct Args {
   int ring;                             // 0, or: positions behind the prefix wrap around after so many slots (one page per sequence)
   int lo_off;                           // 0, or: rows are [hi | lo] bfloat16 terms, lo so many elements behind hi
   int tma, box_rows;                    // the page size suits boxes, of so many slots
+  int n_rows, fill;                     // rows that there are (0: not said); what rows of no tree get: FM_FILL_*
   alignas(64) CUtensorMap map_k, map_v; // the layer's pool as [pages][heads][slots][head_dim], box 64 features x box_rows slots
 };
 
@@ -134,6 +135,7 @@ struct Plan {
   int batch;
   long long total, share;
   bool whole;                           // CTA i takes tile i: nothing is cut
+  bool left;                            // some tree has rows that take no part
 };
 // last sequence whose first unit (tile) is not behind x, and that has any
 template <typename V>
@@ -238,7 +240,7 @@ template <int C, int ROWS, int THREADS>
 __device__ inline void make_plan(const Args& a, Plan& p, int4* info, long long* base, int* tile_base, long long* sh) {
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
   long long carry = 0;
-  int t_carry = 0, longest = 0;
+  int t_carry = 0, longest = 0, left = 0;
   for (int b0 = 0; b0 < a.batch; b0 += THREADS) {
     const int b = b0 + threadIdx.x;
     long long units = 0;
@@ -246,6 +248,9 @@ __device__ inline void make_plan(const Args& a, Plan& p, int4* info, long long* 
     if (b < a.batch) {
       const int4 v = read_sequence(a, b);
       info[b] = v;
+      const int behind = a.row_off[b + 1] - v.x - v.y;       // (more nodes than the caller said)
+      left |= behind != 0;
+      if (behind > 0 && blockIdx.x == 0 && a.status != nullptr) atomicMin(a.status, FM_ERR_CAPACITY);
       const Seq s = sequence<C, ROWS>(a, v);
       tiles = s.tiles * a.Hkv;
       units = (long long)tiles * (s.chunks + OVER);
@@ -272,7 +277,7 @@ __device__ inline void make_plan(const Args& a, Plan& p, int4* info, long long* 
     if (b < a.batch) { base[b] = bx + x - units; tile_base[b] = bt + t - tiles; }
   }
   longest = __reduce_max_sync(0xffffffffu, longest);
-  __syncthreads();
+  p.left = __syncthreads_or(left) != 0;
   if (lane == 0) sh[w] = longest;
   if (threadIdx.x == 0) { base[a.batch] = carry; tile_base[a.batch] = t_carry; }
   __syncthreads();
@@ -284,6 +289,27 @@ __device__ inline void make_plan(const Args& a, Plan& p, int4* info, long long* 
   // Few tiles that are short, or all alike: a CTA each.  (Cutting a tile of up to eight chunks costs more in parts than it gains.)
   const long long most = p.share + (p.share >> 2) > 8 ? p.share + (p.share >> 2) : 8;
   p.whole = t_carry <= (int)gridDim.x && longest <= most;
+}
+// Rows of no tree: in front of the first and behind the last one, and nodes that take no part.  Output 0, lse -inf.
+template <int DH>
+__device__ inline void fill_rows(const Args& a, int lo, int hi) {
+  lo = max(lo, 0);
+  hi = min(hi, a.n_rows);
+  for (int r = lo + blockIdx.x; r < hi; r += gridDim.x) {
+    if (a.fill & FM_FILL_OUT) {
+      uint4* at = reinterpret_cast<uint4*>(static_cast<unsigned short*>(a.out) + r * a.out_row);
+      for (int i = threadIdx.x; i < a.H * (DH / 8); i += blockDim.x) at[i] = make_uint4(0u, 0u, 0u, 0u);
+    }
+    if (a.lse != nullptr && (a.fill & FM_FILL_LSE))
+      for (int i = threadIdx.x; i < a.H; i += blockDim.x) a.lse[(int64_t)r * a.H + i] = -INFINITY;
+  }
+}
+template <int DH>
+__device__ inline void fill(const Args& a, const Plan& p) {  // by all threads
+  fill_rows<DH>(a, 0, a.row_off[0]);
+  fill_rows<DH>(a, a.row_off[a.batch], a.n_rows);
+  if (p.left)
+    for (int b = 0; b < a.batch; ++b) fill_rows<DH>(a, p.info[b].x + p.info[b].y, a.row_off[b + 1]);
 }
 __host__ __device__ constexpr int plan_bytes(int batch) { return 16 * batch + 12 * (batch + 1) + 24; }
 
@@ -515,6 +541,7 @@ __global__ void __launch_bounds__(Rows16<DH>::THREADS, 1) rows16_kernel(const __
   }
   Plan plan;
   make_plan<C, 16, CF::THREADS>(a, plan, s_info, s_base, s_tile_base, s_sh);
+  if (a.fill != 0) fill<DH>(a, plan);
   Walk<C, 16> w;
   w.init(a, plan, blockIdx.x);
   auto wait = [](uint64_t* bar, uint32_t parity) { return __all_sync(0xffffffffu, ptx::mbar_wait(bar, parity)) != 0; };
@@ -960,6 +987,7 @@ __global__ void __launch_bounds__(Rows256<DH>::THREADS, 1) rows256_kernel(const 
   }
   Plan plan;
   make_plan<C, 256, CF::THREADS>(a, plan, s_info, s_base, s_tile_base, s_sh);
+  if (a.fill != 0) fill<DH>(a, plan);
   Walk<C, 256> w;
   w.init(a, plan, blockIdx.x);
   tc::fence_before();

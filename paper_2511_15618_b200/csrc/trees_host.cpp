@@ -139,6 +139,8 @@ PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
     if (want_lse < 0) return nullptr;
     at::Tensor lse;
     if (want_lse) lse = fresh({rows, heads}, q, at::kFloat);
+    t.n_rows = (int32_t)rows;
+    t.fill = (given(a[16]) == nullptr ? FM_FILL_OUT : 0) | (want_lse ? FM_FILL_LSE : 0);       // (what is allocated here holds no stale values)
     t.q = q.data_ptr(); t.k_new = k.data_ptr(); t.v_new = v.data_ptr(); t.out = out.data_ptr();
     t.lse = want_lse ? static_cast<float*>(lse.data_ptr()) : nullptr;
     const size_t bytes = fm_tree_attention_bytes(&c, &t);    // (0: the call itself refuses)

@@ -41,7 +41,8 @@ class FmTreeArgs(C.Structure):
                 ("q_row_stride", C.c_int64), ("new_row_stride", C.c_int64), ("out_row_stride", C.c_int64), ("table", C.c_void_p),
                 ("lens", C.c_void_p), ("seqs", C.c_void_p), ("row_off", C.c_void_p), ("parent", C.c_void_p), ("status", C.c_void_p),
                 ("max_pages", C.c_int32), ("max_seqs", C.c_int32), ("batch", C.c_int32), ("n_heads", C.c_int32), ("max_nodes", C.c_int32),
-                ("max_len", C.c_int32), ("window", C.c_int32), ("n_prefix", C.c_int32), ("scale", C.c_float)]
+                ("max_len", C.c_int32), ("window", C.c_int32), ("n_prefix", C.c_int32), ("scale", C.c_float),
+                ("n_rows", C.c_int32), ("fill", C.c_int32)]
 
 
 _LIB = _HOST = None
@@ -182,7 +183,10 @@ class PagedCache:
 
         q [rows, heads, head_dim], k_new, v_new [rows, kv heads, head_dim] (rows may lie apart); row_off [n + 1]; parent [rows]: an earlier
         node of the tree, counted from its first row, or -1.  seqs [n]: the trees' sequences (None: 0 .. n-1).  max_nodes, max_len:
-        bounds on a tree's nodes and a sequence's positions (default: what there is room for).  Returns out, or (out, lse)."""
+        bounds on a tree's nodes and a sequence's positions (default: what there is room for).  Returns out, or (out, lse).
+
+        A tree of more nodes than max_nodes, or than FM_MAX_TREE_NODES, is recorded for `check`; the nodes behind take no part.  Rows of no tree,
+        theirs and those in front of the first or behind the last tree, are 0, their lse -inf; an `out` that is given keeps them."""
         return _host().attention(*self._at, layer, q, k_new, v_new, row_off, parent, seqs, window, n_prefix, scale, max_nodes, max_len, want_lse, out)
 
 

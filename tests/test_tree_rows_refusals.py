@@ -1,0 +1,13 @@
+"""The rows that an attention call says it has: what is refused without a device."""
+import pytest
+
+import test_tree_refusals as T
+from test_tree_refusals import lib                         # noqa: F401 (the built library)
+
+
+@pytest.mark.parametrize("bad", [dict(n_rows=-1), dict(n_rows=0, fill=1), dict(n_rows=8, fill=4), dict(n_rows=8, fill=-1)])
+def test_rows_and_fills(lib, bad):                         # noqa: F811
+    assert lib.fm_tree_attention_bytes(T.cache(), T.args(n_rows=8, fill=3)) > 0
+    assert lib.fm_tree_attention_bytes(T.cache(), T.args(n_rows=8)) > 0
+    assert lib.fm_tree_attention_bytes(T.cache(), T.args(**bad)) == 0
+    assert lib.fm_tree_attention(T.cache(), 0, T.args(**bad), T.P, 1 << 30, None) == T.INVALID
