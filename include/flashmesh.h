@@ -433,8 +433,9 @@ int fm_device_status(fm_ctx* ctx);
  *   - What only the device sees (an id out of range, an exhausted pool) never leads to an access out
  *     of bounds: the entry concerned is left as it was and, where a call has a status word, the error
  *     is recorded there (DEV int32, 0 = none; of several the lowest code stays; the caller clears it).
- *     Row offsets (row_off) are taken at their word, like the sizes of buffers: they ascend and stay
- *     inside the rows that the caller has.
+ *     Row offsets (row_off) ascend and stay inside the rows that the caller has.  Where a call is told how
+ *     many those are (n_rows; the Python calls always tell), an entry whose offsets do not is one without rows, INVALID_ARG where
+ *     there is a status word; where not, they are taken at their word, like the sizes of buffers.
  *   - A kernel enqueued behind these calls with programmatic stream serialization (its blocks may start
  *     before they end) has to wait for them with griddepcontrol.wait before it touches their buffers.
  *   - A call may be enqueued while earlier ones on the same buffers run on the same stream.  Calls on
@@ -504,11 +505,12 @@ int fm_pages_reserve(const fm_pages* pages, const fm_cache* cache, const int32_t
  * path == NULL: all its rows, in order.  Otherwise rows path[i*path_stride + 0 .. n_acc[i]-1],
  * counted from row_off[i] (an accepted path of a tree).  max_rows: bound on the rows one sequence
  * appends (HOST; beyond 2^30 pieces of 16 bytes in a layer it is lowered to that).  An entry whose pages are not all there, or are shared (no fm_pages_reserve), with a
- * row outside its own or more rows than max_rows is skipped: BAD_STATE or INVALID_ARG in the status
+ * row outside its own or the n_rows that there are, or more rows than max_rows is skipped: BAD_STATE or INVALID_ARG in the status
  * word; its length stays.  Ids as in fm_pages_reserve. */
 typedef struct fm_new_rows {
   const void* k; const void* v;     /* DEV, the type of the cache                                   */
   int64_t layer_stride, row_stride, head_stride;
+  int32_t n_rows;                   /* rows of k and v, or 0: not said                              */
 } fm_new_rows;
 int fm_pages_append(const fm_pages* pages, const fm_cache* cache, const fm_new_rows* rows, const int32_t* seqs /*DEV*/,
                     const int32_t* row_off /*DEV [n+1]*/, const int32_t* path /*DEV or NULL*/, int32_t path_stride,
@@ -534,7 +536,8 @@ int fm_pages_compact(const fm_pages* pages, const fm_cache* cache, int32_t* used
  * A parent that is no earlier node and not -1 takes its node and every node below it out of use:
  * out 0, lse -inf; nobody sees them.  Values of positions and nodes that a row does not see have no
  * effect on it, whatever they hold.  Positions behind the table or max_len are not seen.  A tree of more
- * than max_nodes nodes: CAPACITY in the status word, and the nodes behind take no part.  Their rows, and those in front of row_off[0] and
+ * than max_nodes nodes: CAPACITY in the status word, and the nodes behind take no part.  Offsets that are not inside the n_rows
+ * rows: INVALID_ARG there.  Rows of such nodes, and those in front of row_off[0] and
  * behind row_off[n], are left as they were, or get what `fill` says.
  * Nothing is appended to the cache.  Errors: INVALID_ARG (null pointer, size, stride or alignment),
  * UNSUPPORTED (head_dim not 64 / 128, dtype), CAPACITY (workspace, batch > FM_MAX_TREES, max_nodes > FM_MAX_TREE_NODES). */
@@ -549,7 +552,7 @@ typedef struct fm_tree_args {
   const int32_t* seqs;              /* DEV [batch] rows of table and lens, NULL: 0 .. batch-1; a negative one has no positions */
   const int32_t* row_off;           /* DEV [batch+1]                                                 */
   const int32_t* parent;            /* DEV [rows]                                                    */
-  int32_t* status;                  /* DEV [1] or NULL: CAPACITY (above), INVALID_ARG (a page id that is none, for a position
+  int32_t* status;                  /* DEV [1] or NULL: CAPACITY (above), INVALID_ARG (above; a page id that is none, for a position
                                      * that is seen: its key and value count as zeros), TIMEOUT if a bounded wait gave up */
   int32_t max_pages, max_seqs, batch, n_heads, max_nodes, max_len, window, n_prefix;
   float scale;                      /* above 0                                                       */
@@ -564,10 +567,13 @@ int fm_tree_attention(const fm_cache* cache, int32_t layer, const fm_tree_args* 
  * child whose token is the prediction at the node, as long as there is one.  path: DEV out
  * [batch, path_stride], node indices counted from row_off[i], then -1; n_acc: DEV out [batch]; next_tok:
  * DEV out [batch], the prediction at the last node of the path.  A sequence without rows, or whose
- * node 0 has a parent: n_acc 0, next_tok -1.  Nodes behind path_stride or FM_MAX_TREE_NODES are not followed. */
+ * node 0 has a parent: n_acc 0, next_tok -1.  Nodes behind path_stride or FM_MAX_TREE_NODES are not followed.
+ * fm_tree_accept_rows: the same, told how many rows there are; a sequence whose offsets are not inside them is one without rows. */
 int fm_tree_accept(const int32_t* tokens /*DEV [rows]*/, const int32_t* parent /*DEV*/, const int32_t* row_off /*DEV*/,
                    const int32_t* predicted /*DEV [rows]*/, int32_t batch, int32_t* path, int32_t path_stride, int32_t* n_acc, int32_t* next_tok,
                    void* stream);
+int fm_tree_accept_rows(const int32_t* tokens, const int32_t* parent, const int32_t* row_off, const int32_t* predicted, int32_t rows, int32_t batch,
+                        int32_t* path, int32_t path_stride, int32_t* n_acc, int32_t* next_tok, void* stream);
 
 /* Scores of logits rows x (FM_FP32 / FM_BF16 / FM_FP16, `row_stride` elements apart; e.g. those of
  * fm_verify or fm_draft), one pass over the data:

@@ -277,13 +277,15 @@ int fm_pages_append(const fm_pages* p, const fm_cache* c, const fm_new_rows* row
   if (rc == FM_OK) rc = check_list(seqs, row_off, n);
   if (rc == FM_OK && n > p->max_seqs) rc = FM_ERR_INVALID_ARG;
   if (rc != FM_OK) return rc;
-  if (rows == nullptr || rows->k == nullptr || rows->v == nullptr || !aligned16(rows->k) || !aligned16(rows->v) || max_rows < 0) return FM_ERR_INVALID_ARG;
+  if (rows == nullptr || rows->k == nullptr || rows->v == nullptr || !aligned16(rows->k) || !aligned16(rows->v) || max_rows < 0 || rows->n_rows < 0)
+    return FM_ERR_INVALID_ARG;
   if ((rows->layer_stride | rows->row_stride | rows->head_stride) & 7) return FM_ERR_INVALID_ARG;
   if (path != nullptr && (n_acc == nullptr || path_stride < 1)) return FM_ERR_INVALID_ARG;
   if (n == 0) return FM_OK;
   pg::Rows r;
   r.k = static_cast<const char*>(rows->k); r.v = static_cast<const char*>(rows->v);
   r.layer = 2 * rows->layer_stride; r.row = 2 * rows->row_stride; r.head = 2 * rows->head_stride;
+  r.n_rows = rows->n_rows;
   const int most = 2 * c->n_layers, share = (148 * 3 + n - 1) / n;           // blocks of an entry: a wave over all entries at most
   return launch(pg::append_kernel, dim3(n, share < most ? share : most), 256, 0, as_stream(stream), *p, geo_of(*c), r, seqs, row_off, path, (int)path_stride, n_acc,
                 std::min<int>(max_rows, MOST_PIECES / (c->n_kv_heads * (c->head_dim / 8))));
@@ -338,10 +340,16 @@ int fm_tree_attention(const fm_cache* c, int32_t layer, const fm_tree_args* t, v
 
 int fm_tree_accept(const int32_t* tokens, const int32_t* parent, const int32_t* row_off, const int32_t* predicted, int32_t batch, int32_t* path,
                    int32_t path_stride, int32_t* n_acc, int32_t* next_tok, void* stream) {
+  return fm_tree_accept_rows(tokens, parent, row_off, predicted, INT32_MAX, batch, path, path_stride, n_acc, next_tok, stream);
+}
+
+int fm_tree_accept_rows(const int32_t* tokens, const int32_t* parent, const int32_t* row_off, const int32_t* predicted, int32_t rows, int32_t batch,
+                        int32_t* path, int32_t path_stride, int32_t* n_acc, int32_t* next_tok, void* stream) {
   if (tokens == nullptr || parent == nullptr || row_off == nullptr || predicted == nullptr || path == nullptr || n_acc == nullptr || next_tok == nullptr)
     return FM_ERR_INVALID_ARG;
-  if (batch < 1 || path_stride < 1) return FM_ERR_INVALID_ARG;
-  return launch(tr::accept_kernel, dim3(batch / 4 + (batch % 4 != 0)), 128, 0, as_stream(stream), tokens, parent, row_off, predicted, (int)batch, path, (int)path_stride, n_acc, next_tok);
+  if (rows < 0 || batch < 1 || path_stride < 1) return FM_ERR_INVALID_ARG;
+  return launch(tr::accept_kernel, dim3(batch / 4 + (batch % 4 != 0)), 128, 0, as_stream(stream), tokens, parent, row_off, predicted, (int)batch, (int)rows, path,
+                (int)path_stride, n_acc, next_tok);
 }
 
 int fm_logprobs(const void* logits, int32_t dtype, int32_t rows, int32_t vocab, int64_t row_stride, const int32_t* tokens, float* logprob, float* entropy,

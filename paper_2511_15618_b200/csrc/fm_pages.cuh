@@ -293,12 +293,13 @@ __global__ void __launch_bounds__(256) reserve_copy_kernel(const fm_pages p, con
 struct Rows {
   const char *k, *v;
   int64_t layer, row, head;             // bytes
+  int n_rows;                           // rows that there are, 0: not said
 };
 __global__ void __launch_bounds__(256) append_kernel(const fm_pages p, const Geo g, const Rows rows, const int* seqs, const int* row_off,
                                                      const int* path, int path_stride, const int* n_acc, int max_rows) {
   ptx::grid_dep_wait();
   ptx::grid_dep_launch();
-  const int e = blockIdx.x, s = seqs[e], r0 = row_off[e], own = max(row_off[e + 1] - r0, 0);
+  const int e = blockIdx.x, s = seqs[e], r0 = row_off[e], end = row_off[e + 1], own = r0 >= 0 && end > r0 ? end - r0 : 0;
   const int n = max(path != nullptr ? n_acc[e] : own, 0);
   const int state = entry_state(seqs, e, p.max_seqs);
   if (state != 0) {
@@ -309,7 +310,7 @@ __global__ void __launch_bounds__(256) append_kernel(const fm_pages p, const Geo
   const int* t = p.table + (int64_t)s * p.max_pages;
   // all or nothing: the pages are there and the sequence's own, the rows are its rows
   int bad = 0;
-  if (n > max_rows || r0 < 0 || (path != nullptr && n > path_stride)) bad = 1;
+  if (n > max_rows || r0 < 0 || (rows.n_rows > 0 && end > rows.n_rows) || (path != nullptr && n > path_stride)) bad = 1;
   else if ((int64_t)len + n > (int64_t)p.max_pages * p.page_slots) bad = 2;
   else {
     if (path != nullptr)

@@ -103,10 +103,10 @@ struct Seq {
   int pre, lo;                          // slots [0, pre) and [lo, len) are loaded; both ranges start at a multiple of C
   int n_pre, n_main, chunks, tiles;     // chunks of the two ranges, all chunks, query tiles per kv-head
 };
-__device__ inline int4 read_sequence(const Args& a, int b) {                   // (r0, n, len, seq) from the caller's arrays
-  const int r0 = a.row_off[b], n = a.row_off[b + 1] - r0, seq = a.seqs != nullptr ? a.seqs[b] : b;
+__device__ inline int4 read_sequence(const Args& a, int b) {                   // (r0, n, len, seq) from the caller's arrays; n -1: not rows that there are
+  const int r0 = a.row_off[b], end = a.row_off[b + 1], seq = a.seqs != nullptr ? a.seqs[b] : b;
   const int len = seq >= 0 && seq < a.max_seqs ? max(0, min(a.lens[seq], a.max_len)) : 0;
-  return make_int4(r0, r0 < 0 || n < 0 ? 0 : min(n, a.max_nodes), len, seq);
+  return make_int4(r0, r0 < 0 || end < r0 || (a.n_rows > 0 && end > a.n_rows) ? -1 : min(end - r0, a.max_nodes), len, seq);
 }
 template <int C, int ROWS>
 __device__ inline Seq sequence(const Args& a, int4 v) {
@@ -246,11 +246,12 @@ __device__ inline void make_plan(const Args& a, Plan& p, int4* info, long long* 
     long long units = 0;
     int tiles = 0;
     if (b < a.batch) {
-      const int4 v = read_sequence(a, b);
+      int4 v = read_sequence(a, b);
+      const bool none = v.y < 0, cut = !none && a.row_off[b + 1] - v.x > v.y;        // (cut: more nodes than the caller said)
+      if (none) v.y = 0;
       info[b] = v;
-      const int behind = a.row_off[b + 1] - v.x - v.y;       // (more nodes than the caller said)
-      left |= behind != 0;
-      if (behind > 0 && blockIdx.x == 0 && a.status != nullptr) atomicMin(a.status, FM_ERR_CAPACITY);
+      left |= none || cut;
+      if ((none || cut) && blockIdx.x == 0 && a.status != nullptr) atomicMin(a.status, none ? FM_ERR_INVALID_ARG : FM_ERR_CAPACITY);
       const Seq s = sequence<C, ROWS>(a, v);
       tiles = s.tiles * a.Hkv;
       units = (long long)tiles * (s.chunks + OVER);
@@ -292,24 +293,28 @@ __device__ inline void make_plan(const Args& a, Plan& p, int4* info, long long* 
 }
 // Rows of no tree: in front of the first and behind the last one, and nodes that take no part.  Output 0, lse -inf.
 template <int DH>
-__device__ inline void fill_rows(const Args& a, int lo, int hi) {
-  lo = max(lo, 0);
-  hi = min(hi, a.n_rows);
-  for (int r = lo + blockIdx.x; r < hi; r += gridDim.x) {
-    if (a.fill & FM_FILL_OUT) {
-      uint4* at = reinterpret_cast<uint4*>(static_cast<unsigned short*>(a.out) + r * a.out_row);
-      for (int i = threadIdx.x; i < a.H * (DH / 8); i += blockDim.x) at[i] = make_uint4(0u, 0u, 0u, 0u);
-    }
-    if (a.lse != nullptr && (a.fill & FM_FILL_LSE))
-      for (int i = threadIdx.x; i < a.H; i += blockDim.x) a.lse[(int64_t)r * a.H + i] = -INFINITY;
+__device__ inline void fill_row(const Args& a, int64_t r) {  // by all threads
+  if (a.fill & FM_FILL_OUT) {
+    uint4* at = reinterpret_cast<uint4*>(static_cast<unsigned short*>(a.out) + r * a.out_row);
+    for (int i = threadIdx.x; i < a.H * (DH / 8); i += blockDim.x) at[i] = make_uint4(0u, 0u, 0u, 0u);
   }
+  if (a.lse != nullptr && (a.fill & FM_FILL_LSE))
+    for (int i = threadIdx.x; i < a.H; i += blockDim.x) a.lse[r * a.H + i] = -INFINITY;
 }
 template <int DH>
-__device__ inline void fill(const Args& a, const Plan& p) {  // by all threads
-  fill_rows<DH>(a, 0, a.row_off[0]);
-  fill_rows<DH>(a, a.row_off[a.batch], a.n_rows);
-  if (p.left)
-    for (int b = 0; b < a.batch; ++b) fill_rows<DH>(a, p.info[b].x + p.info[b].y, a.row_off[b + 1]);
+__device__ inline void fill(const Args& a, const Plan& p) {
+  if (!p.left) {                                             // (the trees' rows are neighbours and inside the rows that there are)
+    const int first = a.row_off[0], last = a.row_off[a.batch];
+    for (int64_t r = blockIdx.x; r < first; r += gridDim.x) fill_row<DH>(a, r);
+    for (int64_t r = (int64_t)last + blockIdx.x; r < a.n_rows; r += gridDim.x) fill_row<DH>(a, r);
+    return;
+  }
+  // Some are cut short or none (an error of the caller's): row by row, is it a tree's?
+  for (int64_t r = blockIdx.x; r < a.n_rows; r += gridDim.x) {
+    int in = 0;
+    for (int b = threadIdx.x; b < a.batch; b += blockDim.x) in |= r >= p.info[b].x && r - p.info[b].x < p.info[b].y;
+    if (!__syncthreads_or(in)) fill_row<DH>(a, r);
+  }
 }
 __host__ __device__ constexpr int plan_bytes(int batch) { return 16 * batch + 12 * (batch + 1) + 24; }
 
@@ -1459,12 +1464,14 @@ __device__ inline int walk_path(const int* tokens, const int* parent, const int*
   return at;
 }
 static __global__ void __launch_bounds__(128) accept_kernel(const int* tokens, const int* parent, const int* row_off, const int* predicted, int batch,
-                                                     int* path, int path_stride, int* n_acc, int* next_tok) {
+                                                     int rows, int* path, int path_stride, int* n_acc, int* next_tok) {
   ptx::grid_dep_wait();
   ptx::grid_dep_launch();
   const int b = blockIdx.x * 4 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
   if (b >= batch) return;
-  const int r0 = row_off[b], n = r0 < 0 ? 0 : min(row_off[b + 1] - r0, path_stride);
+  const int from = row_off[b], end = row_off[b + 1];
+  const bool none = from < 0 || end < from || end > rows;    // not rows that there are
+  const int r0 = none ? 0 : from, n = none ? 0 : min(end - from, path_stride);
   int next = -1;
   const int at = walk_path(tokens + r0, parent + r0, predicted + r0, n, lane, next, [&](int i, int node) { path[(int64_t)b * path_stride + i] = node; });
   for (int j = at + lane; j < path_stride; j += 32) path[(int64_t)b * path_stride + j] = -1;

@@ -179,7 +179,7 @@ PyObject* append(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
       n_acc = ids(at_, device, "n_acc: a contiguous int32 tensor on the cache's device");
     }
     const int32_t most = given(a[9]) != nullptr ? number(a[9], "append: max_rows") : (int32_t)(path != nullptr ? stride : k.size(1));
-    const fm_new_rows rows{k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1), k.stride(2)};
+    const fm_new_rows rows{k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1), k.stride(2), (int32_t)k.size(1)};
     const int32_t* s = ids(seqs, device, "seqs: a contiguous int32 tensor on the cache's device");
     const int32_t* o = ids(off, device, "row_off: a contiguous int32 tensor on the cache's device");
     const c10::cuda::CUDAGuard guard((c10::DeviceIndex)device);
@@ -232,14 +232,14 @@ PyObject* accept(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
     const char* const what = "tree_accept: tokens, parent, predicted [rows]; row_off [n + 1]";
     const at::Tensor &tokens = tensor(a[0], what), &parent = tensor(a[1], what), &off = tensor(a[2], what), &predicted = tensor(a[3], what);
     const int64_t rows = tokens.numel(), n = off.numel() - 1;
-    need(tokens.is_cuda() && tokens.dim() == 1 && parent.sizes() == tokens.sizes() && predicted.sizes() == tokens.sizes() && n >= 1 && fits(n), what);
+    need(tokens.is_cuda() && tokens.dim() == 1 && fits(rows) && parent.sizes() == tokens.sizes() && predicted.sizes() == tokens.sizes() && n >= 1 && fits(n), what);
     const int device = tokens.get_device();
     const int32_t stride = given(a[4]) != nullptr ? number(a[4], "tree_accept: max_nodes") : (int32_t)std::min<int64_t>(std::max<int64_t>(rows, 1), FM_MAX_TREE_NODES);
     const int32_t *t = ids(tokens, device, "tokens: a contiguous int32 tensor on one device"), *p = ids(parent, device, "parent: a contiguous int32 tensor on one device"),
                   *o = ids(off, device, "row_off: a contiguous int32 tensor on one device"), *w = ids(predicted, device, "predicted: a contiguous int32 tensor on one device");
     const at::Tensor path = fresh({n, std::max(stride, 0)}, tokens, at::kInt), n_acc = fresh({n}, tokens, at::kInt), next = fresh({n}, tokens, at::kInt);
     const c10::cuda::CUDAGuard guard((c10::DeviceIndex)device);
-    check(fm_tree_accept(t, p, o, w, (int32_t)n, static_cast<int32_t*>(path.data_ptr()), stride, static_cast<int32_t*>(n_acc.data_ptr()),
+    check(fm_tree_accept_rows(t, p, o, w, (int32_t)rows, (int32_t)n, static_cast<int32_t*>(path.data_ptr()), stride, static_cast<int32_t*>(n_acc.data_ptr()),
                          static_cast<int32_t*>(next.data_ptr()), c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)device).stream()), "fm_tree_accept");
     return tuple_of({path, n_acc, next});
   });

@@ -33,7 +33,7 @@ class FmPages(C.Structure):
 
 
 class FmNewRows(C.Structure):
-    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("layer_stride", C.c_int64), ("row_stride", C.c_int64), ("head_stride", C.c_int64)]
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("layer_stride", C.c_int64), ("row_stride", C.c_int64), ("head_stride", C.c_int64), ("n_rows", C.c_int32)]
 
 
 class FmTreeArgs(C.Structure):
@@ -66,6 +66,7 @@ def _lib():
                 ("fm_tree_attention_bytes", C.c_size_t, [cache, C.c_char_p]),
                 ("fm_tree_attention", C.c_int, [cache, i32, C.c_char_p, vp, C.c_size_t, vp]),
                 ("fm_tree_accept", C.c_int, [vp, vp, vp, vp, i32, vp, i32, vp, vp, vp]),
+                ("fm_tree_accept_rows", C.c_int, [vp, vp, vp, vp, i32, i32, vp, i32, vp, vp, vp]),
                 ("fm_logprobs", C.c_int, [vp, i32, i32, i32, i64, vp, vp, vp, vp, i32, vp, vp, vp])):
             getattr(lib, name).restype, getattr(lib, name).argtypes = res, args
         _LIB = lib
@@ -185,7 +186,8 @@ class PagedCache:
         node of the tree, counted from its first row, or -1.  seqs [n]: the trees' sequences (None: 0 .. n-1).  max_nodes, max_len:
         bounds on a tree's nodes and a sequence's positions (default: what there is room for).  Returns out, or (out, lse).
 
-        A tree of more nodes than max_nodes, or than FM_MAX_TREE_NODES, is recorded for `check`; the nodes behind take no part.  Rows of no tree,
+        A tree of more nodes than max_nodes, or than FM_MAX_TREE_NODES, is recorded for `check`; the nodes behind take no part.  So are offsets that do not
+        ascend inside the rows.  Rows of no tree,
         theirs and those in front of the first or behind the last tree, are 0, their lse -inf; an `out` that is given keeps them."""
         return _host().attention(*self._at, layer, q, k_new, v_new, row_off, parent, seqs, window, n_prefix, scale, max_nodes, max_len, want_lse, out)
 

@@ -43,7 +43,7 @@ def agree(c, lens, trees, heads, got, q, kn, vn, at, most):
         want, wl, to, tl = R.attention(q[rows].double().cpu().numpy(), k, v, R.visible(tree[:m], n, 0, 0), c.head_dim ** -0.5, T.UNIT[BF])
         assert (np.abs(got[0][rows].double().cpu().numpy() - want) <= to).all()
         live = ~np.isneginf(wl)
-        assert (np.abs(got[1][rows].double().cpu().numpy() - wl)[live] <= tl[live]).all()
+        assert (np.abs(got[1][rows].double().cpu().numpy()[live] - wl[live]) <= tl[live]).all()
 
 
 @pytest.mark.parametrize("room", ["small", "large"])
@@ -116,3 +116,61 @@ def test_a_captured_call_of_a_padded_batch(room):
         given = [-1, 0, 1, 2] * 2                                        # (a tree that starts inside these: parents that are no earlier nodes)
         agree(c, lens, [given[used[0]:used[1]], given[used[1]:used[2]]], 2, (out, lse), q, kn, vn, used, 256)
     c.check()
+
+
+BAD = [[0, 3, 9], [0, 3, 2 ** 31 - 1], [0, -4, 8], [-1, 3, 8], [5, 3, 8], [-2 ** 31, 2 ** 31 - 1, -2 ** 31], [8, 8, 9], [2 ** 31 - 1, 3, 8], [3, -2 ** 31, 8]]
+
+
+def fits(off, i, rows=8):
+    return 0 <= off[i] <= off[i + 1] <= rows
+
+
+@pytest.mark.parametrize("room", ["small", "large"])
+@pytest.mark.parametrize("off", BAD)
+def test_offsets_that_are_not_inside_the_rows(room, off):
+    """Eight rows; a tree whose rows are not among them is one without rows, the other one is what it is alone."""
+    lens = [70, 33]
+    c, q, kn, vn = case(room, lens, [[-1] * 4, [-1] * 4], 2, 2, 64, 0, 5)
+    parent = [-1, 0, 1, 2, -1, -1, 5, 0]
+    poisoned((q.shape, BF), (q.shape[:2], torch.float32))
+    got = c.attention(0, q, kn, vn, T.dev(off), T.dev(parent), want_lse=True)
+    with pytest.raises(FmError) as e:
+        c.check()
+    assert e.value.code == -1
+    trees = [parent[off[i]:off[i + 1]] if fits(off, i) else [] for i in range(2)]
+    agree(c, lens, trees, 2, got, q, kn, vn, off, 256)
+    rest = [r for r in range(8) if not any(fits(off, i) and off[i] <= r < off[i + 1] for i in range(2))]
+    assert (got[0][rest] == 0).all() and torch.isneginf(got[1][rest]).all()
+
+
+@pytest.mark.parametrize("off", BAD)
+@pytest.mark.parametrize("paths", [False, True])
+def test_appended_offsets_that_are_not_inside_the_rows(off, paths):
+    c = T.PagedCache(2, 20, 4, 1, 64, 2, 10)
+    kn, vn = (torch.randn((2, 8, 1, 64), device="cuda").to(BF) for _ in range(2))
+    c.reserve(T.dev([0, 1]), T.dev([8, 8]))
+    kw = dict(path=T.dev([[0], [0]]), n_acc=T.dev([1, 1])) if paths else {}
+    c.append(T.dev([0, 1]), kn, vn, T.dev(off), **kw)
+    took = [off[i + 1] - off[i] if fits(off, i) else 0 for i in range(2)]
+    took = [min(n, 1) for n in took] if paths else took
+    assert c.lens.tolist() == took
+    for i, n in enumerate(took):
+        for j in range(n):
+            assert torch.equal(c.k[:, c.table[i, j // 4].long(), :, j % 4], kn[:, off[i] + j])
+    # (offsets that descend inside the rows are those of an entry without rows; with a path it names rows that are not its own)
+    if paths or any(off[i] < 0 or off[i + 1] > 8 for i in range(2)):
+        with pytest.raises(FmError) as e:
+            c.check()
+        assert e.value.code == -1
+    else:
+        c.check()
+
+
+@pytest.mark.parametrize("off", BAD)
+def test_accepted_offsets_that_are_not_inside_the_rows(off):
+    tokens, parent, predicted = [1, 2, 3, 4, 1, 2, 3, 4], [-1, 0, 1, 2, -1, -1, 5, 0], [2, 3, 4, 5, 2, 3, 4, 5]
+    path, n_acc, nxt = T.tree_accept(T.dev(tokens), T.dev(parent), T.dev(off), T.dev(predicted))
+    for i in range(2):
+        at = slice(off[i], off[i + 1]) if fits(off, i) else slice(0, 0)
+        want, behind = R.accept(tokens[at], parent[at], predicted[at])
+        assert n_acc[i].item() == len(want) and nxt[i].item() == behind and path[i].tolist() == want + [-1] * (8 - len(want))
