@@ -441,6 +441,7 @@ int fm_device_status(fm_ctx* ctx);
  *   - A call may be enqueued while earlier ones on the same buffers run on the same stream.  Calls on
  *     the same fm_pages, or with the same workspace, from two streams (or two graphs that may run at
  *     the same time) have to be ordered by the caller.
+ *   - These are forms for serving: there is no backward pass.
  *   - Results depend on the arguments alone, to the last bit: the same call gives the same bits.  The
  *     attention of a sequence in other company agrees to rounding (the split of the work follows all lengths).
  * ------------------------------------------------------------------------------------------ */

@@ -5,6 +5,7 @@
 
 #include <ATen/core/LegacyTypeDispatch.h>
 #include <ATen/core/Tensor.h>
+#include <ATen/core/grad_mode.h>
 #include <ATen/ops/empty.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
@@ -53,6 +54,17 @@ inline bool fits(int64_t n) { return n <= std::numeric_limits<int32_t>::max(); }
 inline at::Tensor fresh(std::initializer_list<int64_t> s, const at::Tensor& like, at::ScalarType type) {
   return at::empty(at::IntArrayRef(s.begin(), s.size()), like.options().dtype(type).requires_grad(false));
 }
+// There is no backward pass: a result without a gradient for an input that asks for one would lose it without a word
+inline void no_gradient(const at::Tensor& t) {
+  need(!(t.requires_grad() && at::GradMode::is_enabled()), "an input requires a gradient, and this call has none: call it under torch.no_grad(), or detach the input");
+}
+// in place: what autograd has kept of the tensor for a backward pass is no longer that
+inline void written(const at::Tensor& t) {
+  if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
+inline void all_written(PyObject* const* a, Py_ssize_t first, Py_ssize_t end, const char* what) {
+  for (Py_ssize_t i = first; i < end; ++i) written(tensor(a[i], what));
+}
 inline PyObject* given(PyObject* o) { return o == Py_None ? nullptr : o; }
 
 // f(), with refusals as FmError and torch's errors as torch raises them
@@ -90,6 +102,7 @@ PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
     const int device = number(a[2], "attention: device"), layer = number(a[3], "attention: a number out of range");
     const at::Tensor &q = tensor(a[4], "attention: q"), &k = tensor(a[5], "attention: k_new"), &v = tensor(a[6], "attention: v_new"),
                      &off = tensor(a[7], "attention: row_off"), &parent = tensor(a[8], "attention: parent");
+    for (const at::Tensor* t : {&q, &k, &v}) no_gradient(*t);
     const at::ScalarType type = c.dtype == FM_BF16 ? at::kBFloat16 : at::kHalf;
     const int64_t dh = c.head_dim;
     need(q.dim() == 3 && q.size(0) > 0 && q.size(2) == dh && q.stride(2) == 1 && q.stride(1) == dh && q.scalar_type() == type && lies_on(q, device),
@@ -132,6 +145,7 @@ PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
       out = fresh({rows, heads, dh}, q, type);
     } else {
       out = tensor(a[16], "attention: out");
+      no_gradient(out);
       need(out.sizes() == q.sizes() && out.scalar_type() == type && lies_on(out, device) && out.stride(2) == 1 && out.stride(1) == dh, "attention: out like q");
     }
     t.out_row_stride = rows > 1 ? out.stride(0) : heads * dh;
@@ -149,19 +163,22 @@ PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
     const c10::cuda::CUDAGuard guard((c10::DeviceIndex)device);
     check(fm_tree_attention(&c, layer, &t, bytes > 0 ? work.data_ptr() : nullptr, bytes, c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)device).stream()),
           "fm_tree_attention");
+    if (given(a[16]) != nullptr) written(out);
     if (want_lse) return tuple_of({out, lse});
     return THPVariable_Wrap(out);
   });
 }
 
-// (cache, pages, device, seqs, k_new, v_new, row_off, path, n_acc, max_rows)
+// (cache, pages, device, seqs, k_new, v_new, row_off, path, n_acc, max_rows, tensors that it writes ...)
 PyObject* append(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   return run([&]() -> PyObject* {
-    need(n_args == 10, "append: 10 arguments");
+    need(n_args >= 10, "append: 10 arguments");
     const fm_cache& c = *address<fm_cache>(a[0], "append: cache");
     const fm_pages& p = *address<fm_pages>(a[1], "append: pages");
     const int device = number(a[2], "append: device");
     const at::Tensor &seqs = tensor(a[3], "append: seqs"), &k = tensor(a[4], "append: k_new"), &v = tensor(a[5], "append: v_new"), &off = tensor(a[6], "append: row_off");
+    no_gradient(k);
+    no_gradient(v);
     const int64_t n = seqs.numel();
     need(seqs.dim() == 1 && shaped(off, {n + 1}) && fits(n), "append: seqs [n], row_off [n + 1]");
     const at::ScalarType type = c.dtype == FM_BF16 ? at::kBFloat16 : at::kHalf;
@@ -185,17 +202,18 @@ PyObject* append(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
     const c10::cuda::CUDAGuard guard((c10::DeviceIndex)device);
     check(fm_pages_append(&p, &c, &rows, s, o, path, (int32_t)stride, n_acc, (int32_t)n, most,
                           c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)device).stream()), "fm_pages_append");
+    all_written(a, 10, n_args, "append: a tensor of the cache");
     Py_RETURN_NONE;
   });
 }
 
-// (cache, pages, device, first, second): fork (src, dst), reserve (seqs, grow), truncate (seqs, lens)
+// (cache, pages, device, first, second, tensors that it writes ...): fork (src, dst), reserve (seqs, grow), truncate (seqs, lens)
 enum class Lists { fork, reserve, truncate };
 template <Lists WHICH>
 PyObject* lists(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   return run([&]() -> PyObject* {
     constexpr const char* name = WHICH == Lists::fork ? "fm_pages_fork" : WHICH == Lists::reserve ? "fm_pages_reserve" : "fm_pages_truncate";
-    need(n_args == 5, name);
+    need(n_args >= 5, name);
     const fm_cache& c = *address<fm_cache>(a[0], name);
     const fm_pages& p = *address<fm_pages>(a[1], name);
     const int device = number(a[2], name);
@@ -207,20 +225,22 @@ PyObject* lists(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
     void* stream = c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)device).stream();
     check(WHICH == Lists::fork ? fm_pages_fork(&p, u, v, n, stream) : WHICH == Lists::reserve ? fm_pages_reserve(&p, &c, u, v, n, stream)
                                                                                                : fm_pages_truncate(&p, u, v, n, stream), name);
+    all_written(a, 5, n_args, name);
     Py_RETURN_NONE;
   });
 }
 
-// (cache, pages, device, table): the pages in use
+// (cache, pages, device, table, tensors that it writes ...): the pages in use
 PyObject* compact(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   return run([&]() -> PyObject* {
-    need(n_args == 4, "compact: 4 arguments");
+    need(n_args >= 4, "compact: 4 arguments");
     const fm_cache& c = *address<fm_cache>(a[0], "compact: cache");
     const fm_pages& p = *address<fm_pages>(a[1], "compact: pages");
     const int device = number(a[2], "compact: device");
     const at::Tensor used = fresh({1}, tensor(a[3], "compact: table"), at::kInt);
     const c10::cuda::CUDAGuard guard((c10::DeviceIndex)device);
     check(fm_pages_compact(&p, &c, static_cast<int32_t*>(used.data_ptr()), c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)device).stream()), "fm_pages_compact");
+    all_written(a, 4, n_args, "compact: a tensor of the cache");
     return THPVariable_Wrap(used);
   });
 }
@@ -251,6 +271,7 @@ PyObject* logprobs(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
     need(n_args == 3, "logprobs: 3 arguments");
     const char* const what = "logprobs: logits [rows, vocab] in float32, bfloat16 or float16 on a CUDA device";
     const at::Tensor& x = tensor(a[0], what);
+    no_gradient(x);
     const at::ScalarType type = x.scalar_type();
     const int kind = type == at::kFloat ? FM_FP32 : type == at::kBFloat16 ? FM_BF16 : type == at::kHalf ? FM_FP16 : -1;
     need(kind >= 0 && x.dim() == 2 && x.is_cuda() && x.size(1) >= 1 && (x.stride(1) == 1 || x.size(1) == 1) && fits(x.size(0)) && fits(x.size(1)), what);

@@ -3,7 +3,7 @@
 `PagedCache` owns (or is laid over) the tensors of a pool of cache pages and forwards to the C entry points, by way of native
 functions that check the tensors (csrc/trees_host.cpp); `tree_accept` and `logprobs` are functions of tensors.  Everything is
 enqueued on torch's current stream of the tensors' device, allocates through torch and can be captured into a CUDA graph.
-There is no CPU path.
+There is no CPU path, and no backward pass: an input that requires a gradient is refused where gradients are recorded.
 """
 from __future__ import annotations
 
@@ -127,6 +127,7 @@ class PagedCache:
         types = {torch.bfloat16: FM_BF16, torch.float16: FM_FP16}
         _need(k.dim() == 5 and k.is_cuda and k.dtype in types and k.shape == v.shape and k.dtype == v.dtype and k.device == v.device,
               "PagedCache: k and v [layers, pages, kv heads, slots, head_dim] in bfloat16 or float16 on one device")
+        _need(not (k.requires_grad or v.requires_grad), "PagedCache: keys and values that require a gradient: there is no backward pass")
         _need(k.stride() == v.stride() and k.stride(4) == 1, "PagedCache: k and v with the same strides, the last 1")
         _need(table.dim() == 2 and lens.shape == table.shape[:1] and refs.shape == k.shape[1:2], "PagedCache: table [seqs, pages], lens [seqs], refs [pool]")
         lib = _lib()
@@ -144,6 +145,8 @@ class PagedCache:
         self._pages = FmPages(self.n_pages, self.page_slots, self.max_seqs, self.max_pages, _ids(table, self.device, "table"),
                               _ids(lens, self.device, "lens"), _ids(refs, self.device, "refs"), self.status.data_ptr(), self.work.data_ptr())
         self._at = C.addressof(self._cache), C.addressof(self._pages), self.device.index
+        self._held = table, lens, refs                     # what the calls write: marked as written in place
+        self._all = (k, v) + self._held
 
     def check(self):
         """Waits for the device; raises FmError for the error it has recorded (of several the lowest code), and clears it."""
@@ -156,27 +159,28 @@ class PagedCache:
         """All pages free, all sequences empty."""
         with torch.cuda.device(self.device):
             _check(_lib().fm_pages_reset(C.byref(self._pages), torch.cuda.current_stream().cuda_stream), "fm_pages_reset")
+        torch.autograd.graph.increment_version(self._held)
 
     def fork(self, src, dst):
         """Sequences dst become copies of src that share their pages (int32 lists on the device; negative: skipped)."""
-        _host().fork(*self._at, src, dst)
+        _host().fork(*self._at, src, dst, *self._held)
 
     def reserve(self, seqs, grow):
         """Pages of their own for grow[i] more positions of sequence seqs[i] (a shared last page is copied)."""
-        _host().reserve(*self._at, seqs, grow)
+        _host().reserve(*self._at, seqs, grow, *self._all)
 
     def append(self, seqs, k_new, v_new, row_off, path=None, n_acc=None, max_rows=None):
         """Write rows of k_new, v_new [layers, rows, kv heads, head_dim] behind the sequences and advance their lengths: all rows
         row_off[i]..row_off[i+1]-1 of entry i, or those that path [n, stride] / n_acc [n] name (see `tree_accept`)."""
-        _host().append(*self._at, seqs, k_new, v_new, row_off, path, n_acc, max_rows)
+        _host().append(*self._at, seqs, k_new, v_new, row_off, path, n_acc, max_rows, self.k, self.v, self.lens)
 
     def truncate(self, seqs, lens):
         """Cut sequences seqs[i] to at most lens[i] positions and give back the pages behind them (0: all)."""
-        _host().truncate(*self._at, seqs, lens)
+        _host().truncate(*self._at, seqs, lens, *self._held)
 
     def compact(self):
         """Move the pages in use to the front of the pool; returns their number (int32 [1], on the device)."""
-        return _host().compact(*self._at, self.table)
+        return _host().compact(*self._at, self.table, *self._all)
 
     def attention(self, layer, q, k_new, v_new, row_off, parent, seqs=None, window=0, n_prefix=0, scale=None, max_nodes=None, max_len=None,
                   want_lse=False, out=None):
