@@ -105,7 +105,7 @@ PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
     for (const at::Tensor* t : {&q, &k, &v}) no_gradient(*t);
     const at::ScalarType type = c.dtype == FM_BF16 ? at::kBFloat16 : at::kHalf;
     const int64_t dh = c.head_dim;
-    need(q.dim() == 3 && q.size(0) > 0 && q.size(2) == dh && q.stride(2) == 1 && q.stride(1) == dh && q.scalar_type() == type && lies_on(q, device),
+    need(q.dim() == 3 && q.size(2) == dh && q.stride(2) == 1 && q.stride(1) == dh && q.scalar_type() == type && lies_on(q, device),
          "attention: q [rows, heads, head_dim] of the cache's type");
     const int64_t rows = q.size(0), heads = q.size(1), n = off.numel() - 1;
     need(shaped(k, {rows, c.n_kv_heads, dh}) && k.sizes() == v.sizes() && k.strides() == v.strides() && k.stride(2) == 1 && k.stride(1) == dh &&
@@ -118,7 +118,7 @@ PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
       need(shaped(s, {n}), "attention: seqs [n]");
       seqs = ids(s, device, "seqs: a contiguous int32 tensor on the cache's device");
     }
-    need(n >= 1 && shaped(parent, {rows}) && (seqs != nullptr || n <= p.max_seqs) && fits(n) && fits(rows) && fits(heads),
+    need((n >= 1 || (n == 0 && rows == 0)) && shaped(parent, {rows}) && (seqs != nullptr || n <= p.max_seqs) && fits(n) && fits(rows) && fits(heads),
          "attention: row_off [n + 1], parent [rows], seqs [n]");
     const char* const range = "attention: a number out of range";
     fm_tree_args t{};
@@ -153,6 +153,10 @@ PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
     if (want_lse < 0) return nullptr;
     at::Tensor lse;
     if (want_lse) lse = fresh({rows, heads}, q, at::kFloat);
+    if (rows == 0) {                                         // (no tree has a node)
+      if (want_lse) return tuple_of({out, lse});
+      return THPVariable_Wrap(out);
+    }
     t.n_rows = (int32_t)rows;
     t.fill = (given(a[16]) == nullptr ? FM_FILL_OUT : 0) | (want_lse ? FM_FILL_LSE : 0);       // (what is allocated here holds no stale values)
     t.q = q.data_ptr(); t.k_new = k.data_ptr(); t.v_new = v.data_ptr(); t.out = out.data_ptr();
@@ -195,8 +199,10 @@ PyObject* append(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
       path = ids(pt, device, "path: a contiguous int32 tensor on the cache's device");
       n_acc = ids(at_, device, "n_acc: a contiguous int32 tensor on the cache's device");
     }
-    const int32_t most = given(a[9]) != nullptr ? number(a[9], "append: max_rows") : (int32_t)(path != nullptr ? stride : k.size(1));
-    const fm_new_rows rows{k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1), k.stride(2), (int32_t)k.size(1)};
+    int32_t most = given(a[9]) != nullptr ? number(a[9], "append: max_rows") : (int32_t)(path != nullptr ? stride : k.size(1));
+    const bool none = k.size(1) == 0;                        // no rows, and tensors without an address: entries may append nothing
+    if (none) most = std::min(most, 0);
+    const fm_new_rows rows{none ? c.k : k.data_ptr(), none ? c.v : v.data_ptr(), k.stride(0), k.stride(1), k.stride(2), (int32_t)k.size(1)};
     const int32_t* s = ids(seqs, device, "seqs: a contiguous int32 tensor on the cache's device");
     const int32_t* o = ids(off, device, "row_off: a contiguous int32 tensor on the cache's device");
     const c10::cuda::CUDAGuard guard((c10::DeviceIndex)device);
@@ -252,12 +258,14 @@ PyObject* accept(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
     const char* const what = "tree_accept: tokens, parent, predicted [rows]; row_off [n + 1]";
     const at::Tensor &tokens = tensor(a[0], what), &parent = tensor(a[1], what), &off = tensor(a[2], what), &predicted = tensor(a[3], what);
     const int64_t rows = tokens.numel(), n = off.numel() - 1;
-    need(tokens.is_cuda() && tokens.dim() == 1 && fits(rows) && parent.sizes() == tokens.sizes() && predicted.sizes() == tokens.sizes() && n >= 1 && fits(n), what);
+    need(tokens.is_cuda() && tokens.dim() == 1 && fits(rows) && parent.sizes() == tokens.sizes() && predicted.sizes() == tokens.sizes() && n >= 0 && fits(n), what);
     const int device = tokens.get_device();
     const int32_t stride = given(a[4]) != nullptr ? number(a[4], "tree_accept: max_nodes") : (int32_t)std::min<int64_t>(std::max<int64_t>(rows, 1), FM_MAX_TREE_NODES);
     const int32_t *t = ids(tokens, device, "tokens: a contiguous int32 tensor on one device"), *p = ids(parent, device, "parent: a contiguous int32 tensor on one device"),
                   *o = ids(off, device, "row_off: a contiguous int32 tensor on one device"), *w = ids(predicted, device, "predicted: a contiguous int32 tensor on one device");
+    if (rows == 0) t = p = w = o;                            // (tensors without an address; no tree has a node to read)
     const at::Tensor path = fresh({n, std::max(stride, 0)}, tokens, at::kInt), n_acc = fresh({n}, tokens, at::kInt), next = fresh({n}, tokens, at::kInt);
+    if (n == 0) return tuple_of({path, n_acc, next});
     const c10::cuda::CUDAGuard guard((c10::DeviceIndex)device);
     check(fm_tree_accept_rows(t, p, o, w, (int32_t)rows, (int32_t)n, static_cast<int32_t*>(path.data_ptr()), stride, static_cast<int32_t*>(n_acc.data_ptr()),
                          static_cast<int32_t*>(next.data_ptr()), c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)device).stream()), "fm_tree_accept");
