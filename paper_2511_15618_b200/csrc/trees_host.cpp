@@ -50,6 +50,14 @@ inline int32_t* ids(const at::Tensor& t, int device, const char* what) {
   return static_cast<int32_t*>(t.data_ptr());
 }
 inline bool shaped(const at::Tensor& t, std::initializer_list<int64_t> s) { return t.sizes().equals(at::IntArrayRef(s.begin(), s.size())); }
+// (the stride of a dimension of size 1 means nothing, and differs between views of the same contents)
+inline int64_t step(const at::Tensor& t, int64_t d, int64_t otherwise) { return t.size(d) > 1 ? t.stride(d) : otherwise; }
+inline bool alike(const at::Tensor& x, const at::Tensor& y) {
+  if (!x.sizes().equals(y.sizes())) return false;
+  for (int64_t d = 0; d < x.dim(); ++d)
+    if (step(x, d, 0) != step(y, d, 0)) return false;
+  return true;
+}
 inline bool fits(int64_t n) { return n <= std::numeric_limits<int32_t>::max(); }
 inline at::Tensor fresh(std::initializer_list<int64_t> s, const at::Tensor& like, at::ScalarType type) {
   return at::empty(at::IntArrayRef(s.begin(), s.size()), like.options().dtype(type).requires_grad(false));
@@ -105,10 +113,10 @@ PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
     for (const at::Tensor* t : {&q, &k, &v}) no_gradient(*t);
     const at::ScalarType type = c.dtype == FM_BF16 ? at::kBFloat16 : at::kHalf;
     const int64_t dh = c.head_dim;
-    need(q.dim() == 3 && q.size(2) == dh && q.stride(2) == 1 && q.stride(1) == dh && q.scalar_type() == type && lies_on(q, device),
+    need(q.dim() == 3 && q.size(2) == dh && q.stride(2) == 1 && step(q, 1, dh) == dh && q.scalar_type() == type && lies_on(q, device),
          "attention: q [rows, heads, head_dim] of the cache's type");
     const int64_t rows = q.size(0), heads = q.size(1), n = off.numel() - 1;
-    need(shaped(k, {rows, c.n_kv_heads, dh}) && k.sizes() == v.sizes() && k.strides() == v.strides() && k.stride(2) == 1 && k.stride(1) == dh &&
+    need(shaped(k, {rows, c.n_kv_heads, dh}) && alike(k, v) && k.stride(2) == 1 && step(k, 1, dh) == dh &&
              k.scalar_type() == type && v.scalar_type() == type && lies_on(k, device) && lies_on(v, device),
          "attention: k_new and v_new [rows, kv heads, head_dim] of the cache's type, with the same strides");
     PyObject* const listed = given(a[9]);
@@ -137,18 +145,17 @@ PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
     t.table = p.table; t.lens = p.lens; t.status = p.status; t.seqs = seqs;
     t.row_off = ids(off, device, "row_off: a contiguous int32 tensor on the cache's device");
     t.parent = ids(parent, device, "parent: a contiguous int32 tensor on the cache's device");
-    // (a single row has no distance to the next one that matters)
-    t.q_row_stride = rows > 1 ? q.stride(0) : heads * dh;
-    t.new_row_stride = rows > 1 ? k.stride(0) : c.n_kv_heads * dh;
+    t.q_row_stride = step(q, 0, heads * dh);
+    t.new_row_stride = step(k, 0, c.n_kv_heads * dh);
     at::Tensor out;
     if (given(a[16]) == nullptr) {
       out = fresh({rows, heads, dh}, q, type);
     } else {
       out = tensor(a[16], "attention: out");
       no_gradient(out);
-      need(out.sizes() == q.sizes() && out.scalar_type() == type && lies_on(out, device) && out.stride(2) == 1 && out.stride(1) == dh, "attention: out like q");
+      need(out.sizes() == q.sizes() && out.scalar_type() == type && lies_on(out, device) && out.stride(2) == 1 && step(out, 1, dh) == dh, "attention: out like q");
     }
-    t.out_row_stride = rows > 1 ? out.stride(0) : heads * dh;
+    t.out_row_stride = step(out, 0, heads * dh);
     const int want_lse = PyObject_IsTrue(a[15]);
     if (want_lse < 0) return nullptr;
     at::Tensor lse;
@@ -186,7 +193,7 @@ PyObject* append(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
     const int64_t n = seqs.numel();
     need(seqs.dim() == 1 && shaped(off, {n + 1}) && fits(n), "append: seqs [n], row_off [n + 1]");
     const at::ScalarType type = c.dtype == FM_BF16 ? at::kBFloat16 : at::kHalf;
-    need(k.dim() == 4 && k.size(0) == c.n_layers && k.size(2) == c.n_kv_heads && k.size(3) == c.head_dim && k.sizes() == v.sizes() && k.strides() == v.strides() &&
+    need(k.dim() == 4 && k.size(0) == c.n_layers && k.size(2) == c.n_kv_heads && k.size(3) == c.head_dim && alike(k, v) &&
              k.stride(3) == 1 && k.scalar_type() == type && v.scalar_type() == type && lies_on(k, device) && lies_on(v, device) && fits(k.size(1)),
          "append: k_new and v_new [layers, rows, kv heads, head_dim] of the cache's type, with the same strides");
     need((given(a[7]) == nullptr) == (given(a[8]) == nullptr), "append: path and n_acc go together");
@@ -202,7 +209,7 @@ PyObject* append(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
     int32_t most = given(a[9]) != nullptr ? number(a[9], "append: max_rows") : (int32_t)(path != nullptr ? stride : k.size(1));
     const bool none = k.size(1) == 0;                        // no rows, and tensors without an address: entries may append nothing
     if (none) most = std::min(most, 0);
-    const fm_new_rows rows{none ? c.k : k.data_ptr(), none ? c.v : v.data_ptr(), k.stride(0), k.stride(1), k.stride(2), (int32_t)k.size(1)};
+    const fm_new_rows rows{none ? c.k : k.data_ptr(), none ? c.v : v.data_ptr(), step(k, 0, 0), step(k, 1, 0), step(k, 2, 0), (int32_t)k.size(1)};
     const int32_t* s = ids(seqs, device, "seqs: a contiguous int32 tensor on the cache's device");
     const int32_t* o = ids(off, device, "row_off: a contiguous int32 tensor on the cache's device");
     const c10::cuda::CUDAGuard guard((c10::DeviceIndex)device);
