@@ -150,6 +150,7 @@ class PagedCache:
 
     def check(self):
         """Waits for the device; raises FmError for the error it has recorded (of several the lowest code), and clears it."""
+        torch.cuda.synchronize(self.device)                # (calls on any of its streams)
         code = int(self.status.item())
         if code != 0:
             self.status.zero_()
