@@ -1473,8 +1473,12 @@ int tree_attention(fm_ctx* c, int level, const LayerDev& L, const bf16* k_new, c
   fc.k = L.K; fc.v = L.V; fc.page_stride = a.page; fc.head_stride = a.head; fc.slot_stride = a.slot;
   fc.n_layers = 1; fc.n_pages = dm.max_batch; fc.page_slots = slots; fc.n_kv_heads = dm.Hkv; fc.head_dim = dm.dh; fc.dtype = FM_BF16;
   a.tma = tr::make_maps(fc, 0, 1, a) ? 1 : 0;
-  c->launches += 2;
-  return tr::launch(a, FM_BF16, dm.dh, c->stream);
+  const long pi = prof_open(c, PROF_ATTN, 0.0);
+  const int rc = tr::launch(a, FM_BF16, dm.dh, c->stream);
+  prof_close(c, pi);
+  if (rc == FM_OK) c->launches += tr::launches(a, dm.dh);
+  if (c->debug_sync) debug_sync_check(c, "tree attention");
+  return rc;
 }
 
 void tree_stack(fm_ctx* c, int R, int s, int first_layer, const float* next_gain, bool want_a, float* z) {
@@ -1495,7 +1499,10 @@ void tree_stack(fm_ctx* c, int R, int s, int first_layer, const float* next_gain
     eq.dm = dm; eq.rows = t.row[level]; eq.level = level; eq.rope = c->rope_tab; eq.qscale = (float)(1.4426950408889634 / sqrt((double)dm.dh));
     eq.q = pr.q; eq.kbuf = kn; eq.vbuf = vn;
     pf_gemm(c, pf::PF_QKV, L.Wqkv, pr.a, ld, qkvw, d, R, eq);
-    if (c->launch_error == FM_OK) c->launch_error = tree_attention(c, level, L, kn, vn);
+    if (c->launch_error == FM_OK) {
+      const int rc = tree_attention(c, level, L, kn, vn);
+      if (rc != FM_OK) c->launch_error = rc;
+    }
     tc::Epi eo{};
     eo.x = x; eo.ldx = d; eo.add = 1; eo.gain = L.g2; eo.a_out = pr.a; eo.lda = 2 * d; eo.lo_off = d; eo.ssq_out = pr.ssq; eo.ld_ssq_out = c->ssq_ld;
     gemm(c, L.Wo, pad128(d), 0, pr.attn, ld, 0, d, hd, R, nullptr, tc::EPI_RESID, eo, 2);

@@ -232,6 +232,10 @@ size_t workspace_bytes(int max_nodes, int group, int head_dim) {             // 
 bool make_maps(const fm_cache& c, int layer, int max_pages, Args& a) {
   return make_maps_of(c, layer, max_pages, few_rows(a, c.head_dim) && c.head_dim == 128 ? tr::Rows16<128>::C : 128, a);
 }
+int launches(const Args& a, int head_dim) {
+  const bool few = few_rows(a, head_dim);
+  return whole_for_sure(a, few ? 16 : 256, few && head_dim == 128 ? Rows16<128>::C : 128, SMS) ? 1 : 2;
+}
 int launch(const Args& a, int dtype, int head_dim, cudaStream_t stream) {
   if (dtype == FM_BF16) return head_dim == 64 ? tree_attention<bf16, 64>(a, stream) : tree_attention<bf16, 128>(a, stream);
   return head_dim == 64 ? tree_attention<__half, 64>(a, stream) : tree_attention<__half, 128>(a, stream);

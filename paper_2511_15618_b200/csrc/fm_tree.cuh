@@ -1483,6 +1483,7 @@ constexpr size_t DESC_BYTES = 8192;      // in front of a workspace's parts: wha
 size_t workspace_bytes(int max_nodes, int group, int head_dim);
 bool make_maps(const fm_cache& c, int layer, int max_pages, Args& a);          // the sizes in `a` are set
 int launch(const Args& a, int dtype, int head_dim, cudaStream_t stream);
+int launches(const Args& a, int head_dim);                   // of kernels, by that: two where a tile may be cut
 Div div_by(int d);
 
 }  // namespace tr
