@@ -1,6 +1,7 @@
 """Compile the CUDA library in-tree for sm_100a with nvcc, and the functions that call it with torch tensors (no GPU needed to build)."""
 from __future__ import annotations
 
+import importlib.metadata
 import importlib.util
 import os
 import subprocess
@@ -18,12 +19,22 @@ HOST = os.path.join(HERE, "_trees.so")
 HOST_SRC = os.path.join(HERE, "csrc", "trees_host.cpp")
 
 
+def _built_for():
+    """What _trees.so is compiled and linked against, as it is written into the module: another torch or Python may have other
+    layouts and symbols, whatever the files' times."""
+    try:
+        torch = importlib.metadata.version("torch")
+    except importlib.metadata.PackageNotFoundError:        # (a source tree on the path)
+        torch = os.path.dirname(importlib.util.find_spec("torch").origin)
+    return f"fm built for torch {torch}, {sysconfig.get_config_var('SOABI')};"
+
+
 def _host_command():
     torch = os.path.dirname(importlib.util.find_spec("torch").origin)
     cuda = os.path.join(os.environ.get("CUDA_HOME", "/usr/local/cuda"), "include")
     include = [os.path.join(torch, "include"), os.path.join(torch, "include", "torch", "csrc", "api", "include"), sysconfig.get_paths()["include"], cuda]
     libs = os.path.join(torch, "lib")
-    return (["g++", "-O2", "-std=c++17", "-fPIC", "-shared"] + ["-I" + d for d in include] + ["-o", HOST, HOST_SRC, "-L" + HERE, "-l:libflashmesh.so", "-L" + libs,
+    return (["g++", "-O2", "-std=c++17", "-fPIC", "-shared", f'-DFM_BUILT_FOR="{_built_for()}"'] + ["-I" + d for d in include] + ["-o", HOST, HOST_SRC, "-L" + HERE, "-l:libflashmesh.so", "-L" + libs,
             "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_python", "-Wl,-rpath,$ORIGIN"])
 
 
@@ -39,6 +50,14 @@ def _newer(target, sources):
     return os.path.exists(target) and all(os.path.getmtime(s) <= os.path.getmtime(target) for s in sources)
 
 
+def _host_fits():
+    """Is _trees.so there, newer than its sources and built for this torch and Python?"""
+    if not _newer(HOST, [HOST_SRC, _sources()[0]]):
+        return False
+    with open(HOST, "rb") as f:
+        return _built_for().encode() in f.read()
+
+
 def _sources():
     out = [os.path.join(HERE, "..", "include", "flashmesh.h")]
     for f in os.listdir(os.path.join(HERE, "csrc")):
@@ -48,13 +67,14 @@ def _sources():
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
-    """Build libflashmesh.so and _trees.so if they are missing or older than a source file; return the library's path."""
+    """Build libflashmesh.so and _trees.so if they are missing or older than a source file (the latter also if it is for another torch or
+    Python); return the library's path."""
     if force or not _newer(LIB, _sources()):
         nvcc = os.environ.get("NVCC", "nvcc")
         res = _run([nvcc] + NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else []) + ["-o", LIB] + SRC, "nvcc failed building libflashmesh.so")
         if verbose:
             sys.stderr.write(res.stderr)
-    if force or not _newer(HOST, [HOST_SRC, _sources()[0]]):
+    if force or not _host_fits():
         _run(_host_command(), "g++ failed building _trees.so")
     return LIB
 

@@ -325,7 +325,10 @@ PyMethodDef methods[] = {
     fast("truncate", lists<Lists::truncate>), fast("compact", compact), fast("accept", accept), fast("logprobs", logprobs),
     {"set_error", set_error, METH_O, nullptr},
     {nullptr, nullptr, 0, nullptr}};
-PyModuleDef module = {PyModuleDef_HEAD_INIT, "_trees", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
+#ifndef FM_BUILT_FOR
+#define FM_BUILT_FOR "fm built for: not said"
+#endif
+PyModuleDef module = {PyModuleDef_HEAD_INIT, "_trees", FM_BUILT_FOR, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
 
