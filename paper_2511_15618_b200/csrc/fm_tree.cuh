@@ -97,6 +97,12 @@ __device__ inline void cp_arrive(uint64_t* bar) {            // when this thread
   asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(ptx::smem_u32(bar)) : "memory");
 }
 
+// Exponentials are taken to a reference so many powers of two below the row's maximum; sums and outputs carry the same factor.  Half
+// has no number between 0 and 2^-24: weights of an unshifted softmax below 2^-25 would vanish from the product with the values
+// and those below 2^-14 lose bits, and in a long cache all of a row but its sink can be such.  A shift of 14 keeps weights down to 2^-28 of
+// the largest at full precision and 2^-39 at all (2^14 times a value fits fp32 sums).  bfloat16 has fp32's exponents.
+template <typename T> constexpr float SHIFT = __is_same(T, bf16) ? 0.f : 14.f;
+
 // ---- what a sequence asks for
 struct Seq {
   int r0, n, len, seq;                  // first row, nodes, cached positions, its row of the table
@@ -707,7 +713,7 @@ __global__ void __launch_bounds__(Rows16<DH>::THREADS, 1) rows16_kernel(const __
           for (int nt = 0; nt < NT; ++nt) mx = fmaxf(mx, fmaxf(sc[nt][hr * 2], sc[nt][hr * 2 + 1]));
           mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
           mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
-          const float mnew = fmaxf(mrun[hr], mx * a.scale_log2);
+          const float mnew = fmaxf(mrun[hr], fmaf(mx, a.scale_log2, -SHIFT<T>));
           base[hr] = mnew == -INFINITY ? 0.f : mnew;
           scale[hr] = mnew == mrun[hr] ? 1.f : ex2(mrun[hr] - base[hr]);
           mrun[hr] = mnew;
@@ -860,8 +866,8 @@ __global__ void __launch_bounds__(Rows16<DH>::THREADS, 1) rows16_kernel(const __
 // half of them and every chunk to both (keys and values are loaded once for 256 rows); one of up to 128 rows gives its
 // chunks to the slots alternately, and their outputs are merged at the end.  Steps are numbered through: slot = step mod 2.
 // Exponentials are taken to the maximum in use, that of the row's first chunk, and the scores' maximum beside them: only when it
-// exceeds the one in use by more than P's type holds (2^40 for bfloat16, 2^12 for half) the output is rescaled and the
-// chunk's exponentials are taken again.  (The maximum first, then the exponentials: a step of a slot took 4200 clocks, 560
+// exceeds the one in use by more than P's type holds (2^40 for bfloat16, 2^5 for half, whose weights start at 2^10: see SHIFT) the output
+// is rescaled and the chunk's exponentials are taken again.  (The maximum first, then the exponentials: a step of a slot took 4200 clocks, 560
 // of them for the maximum.)
 // One warp brings keys, one values, each as soon as its place is free (keys once their scores are multiplied); a third
 // one (the fixer) brings queries and takes values that are not finite out of chunks with hidden keys.  What threads write is
@@ -882,7 +888,9 @@ struct Rows256 {
   static constexpr int FIXED = 2 * Q + STAGES * STAGE + (int)sizeof(Tree) + 2 * 128 * 8 + 512 + 1024;
   static int bytes(int batch) { return FIXED + plan_bytes(batch); }
 };
-template <typename T> constexpr float HEADROOM = __is_same(T, bf16) ? 40.f : 12.f;      // log2 of what P may grow to
+// log2 of what P may grow to, and of what it starts at: of half's 40 powers of two 5 for growth, 35 below the first chunk's maximum
+template <typename T> constexpr float HEADROOM = __is_same(T, bf16) ? 40.f : 15.f;
+template <typename T> constexpr float START = __is_same(T, bf16) ? 0.f : 10.f;
 
 __device__ inline uint64_t pack2(float a, float b) {
   uint64_t r;
@@ -1188,7 +1196,7 @@ __global__ void __launch_bounds__(Rows256<DH>::THREADS, 1) rows256_kernel(const 
 #pragma unroll
             for (int u = 0; u < 4; ++u) m4[u] = max3(m4[u], __uint_as_float(x[j + 2 * u]), __uint_as_float(x[j + 2 * u + 1]));
         };
-        auto row_max = [&] { return fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * sc; };
+        auto row_max = [&] { return fmaf(fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])), sc, -START<T>); };
         if (!any) {                                          // the row's first chunk: its maximum first
           ld32(tS, r[0]);
 #pragma unroll
@@ -1218,7 +1226,7 @@ __global__ void __launch_bounds__(Rows256<DH>::THREADS, 1) rows256_kernel(const 
           const float2 sa = unpack2(sums[0]), sb = unpack2(sums[1]);
           sum = (sa.x + sa.y) + (sb.x + sb.y);
           const float mx = row_max();
-          const bool over = mx > m + HEADROOM<T> || (m == -INFINITY && mx != -INFINITY);
+          const bool over = mx > m + (HEADROOM<T> - START<T>) || (m == -INFINITY && mx != -INFINITY);
           if (!__any_sync(0xffffffffu, over)) break;
           // seldom: rescale to the new maximum (the scores' arrival says that the slot's last product is in) and again
           const float mn = over ? mx : m, f = m == -INFINITY ? (over ? 0.f : 1.f) : ex2(m - mn);
