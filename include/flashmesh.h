@@ -533,7 +533,7 @@ int fm_pages_compact(const fm_pages* pages, const fm_cache* cache, int32_t* used
  *   window > 0: of both only what lies less than `window` positions before it, and always the
  *   positions s < n_prefix (conditioning).
  * out = sum p v, p = softmax(scale q k), sums and softmax in 32 bits (p is rounded to the cache's type for its
- * product with v; in half precision what is below 2^-35 of the row's largest p rounds to nothing there); lse = log sum exp(scale q k).
+ * product with v; in half precision what is below 2^-34 of the row's largest p rounds to nothing there); lse = log sum exp(scale q k).
  * A parent that is no earlier node and not -1 takes its node and every node below it out of use:
  * out 0, lse -inf; nobody sees them.  Values of positions and nodes that a row does not see have no
  * effect on it, whatever they hold.  Positions behind the table or max_len are not seen.  A tree of more

@@ -307,10 +307,13 @@ __device__ inline void fill_row(const Args& a, int64_t r) {  // by all threads
   if (a.lse != nullptr && (a.fill & FM_FILL_LSE))
     for (int i = threadIdx.x; i < a.H; i += blockDim.x) a.lse[r * a.H + i] = -INFINITY;
 }
+// first row of the first tree, and of none behind the last (read before the plan is made: its loads hide these)
+__device__ inline int2 ends_of(const Args& a) { return a.fill != 0 ? make_int2(a.row_off[0], a.row_off[a.batch]) : make_int2(0, 0); }
+__device__ inline bool to_fill(const Args& a, const Plan& p, int2 ends) { return a.fill != 0 && (p.left || ends.x > 0 || ends.y < a.n_rows); }
 template <int DH>
-__device__ inline void fill(const Args& a, const Plan& p) {
+__device__ inline void fill(const Args& a, const Plan& p, int2 ends) {
   if (!p.left) {                                             // (the trees' rows are neighbours and inside the rows that there are)
-    const int first = a.row_off[0], last = a.row_off[a.batch];
+    const int first = ends.x, last = ends.y;
     for (int64_t r = blockIdx.x; r < first; r += gridDim.x) fill_row<DH>(a, r);
     for (int64_t r = (int64_t)last + blockIdx.x; r < a.n_rows; r += gridDim.x) fill_row<DH>(a, r);
     return;
@@ -551,8 +554,9 @@ __global__ void __launch_bounds__(Rows16<DH>::THREADS, 1) rows16_kernel(const __
     ptx::fence_mbar_init();
   }
   Plan plan;
+  const int2 ends = ends_of(a);
   make_plan<C, 16, CF::THREADS>(a, plan, s_info, s_base, s_tile_base, s_sh);
-  if (a.fill != 0) fill<DH>(a, plan);
+  if (to_fill(a, plan, ends)) fill<DH>(a, plan, ends);
   Walk<C, 16> w;
   w.init(a, plan, blockIdx.x);
   auto wait = [](uint64_t* bar, uint32_t parity) { return __all_sync(0xffffffffu, ptx::mbar_wait(bar, parity)) != 0; };
@@ -866,7 +870,7 @@ __global__ void __launch_bounds__(Rows16<DH>::THREADS, 1) rows16_kernel(const __
 // half of them and every chunk to both (keys and values are loaded once for 256 rows); one of up to 128 rows gives its
 // chunks to the slots alternately, and their outputs are merged at the end.  Steps are numbered through: slot = step mod 2.
 // Exponentials are taken to the maximum in use, that of the row's first chunk, and the scores' maximum beside them: only when it
-// exceeds the one in use by more than P's type holds (2^40 for bfloat16, 2^5 for half, whose weights start at 2^10: see SHIFT) the output
+// exceeds the one in use by more than P's type holds (2^40 for bfloat16, 2^6.5 for half, whose weights start at 2^9: see SHIFT) the output
 // is rescaled and the chunk's exponentials are taken again.  (The maximum first, then the exponentials: a step of a slot took 4200 clocks, 560
 // of them for the maximum.)
 // One warp brings keys, one values, each as soon as its place is free (keys once their scores are multiplied); a third
@@ -888,9 +892,9 @@ struct Rows256 {
   static constexpr int FIXED = 2 * Q + STAGES * STAGE + (int)sizeof(Tree) + 2 * 128 * 8 + 512 + 1024;
   static int bytes(int batch) { return FIXED + plan_bytes(batch); }
 };
-// log2 of what P may grow to, and of what it starts at: of half's 40 powers of two 5 for growth, 35 below the first chunk's maximum
-template <typename T> constexpr float HEADROOM = __is_same(T, bf16) ? 40.f : 15.f;
-template <typename T> constexpr float START = __is_same(T, bf16) ? 0.f : 10.f;
+// log2 of what P may grow to, and of what it starts at: of half's 40 powers of two 6.5 for growth, 34 below the first chunk's maximum
+template <typename T> constexpr float HEADROOM = __is_same(T, bf16) ? 40.f : 15.5f;
+template <typename T> constexpr float START = __is_same(T, bf16) ? 0.f : 9.f;
 
 __device__ inline uint64_t pack2(float a, float b) {
   uint64_t r;
@@ -999,8 +1003,9 @@ __global__ void __launch_bounds__(Rows256<DH>::THREADS, 1) rows256_kernel(const 
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   Plan plan;
+  const int2 ends = ends_of(a);
   make_plan<C, 256, CF::THREADS>(a, plan, s_info, s_base, s_tile_base, s_sh);
-  if (a.fill != 0) fill<DH>(a, plan);
+  if (to_fill(a, plan, ends)) fill<DH>(a, plan, ends);
   Walk<C, 256> w;
   w.init(a, plan, blockIdx.x);
   tc::fence_before();
