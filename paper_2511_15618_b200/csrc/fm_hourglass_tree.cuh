@@ -155,13 +155,13 @@ static __global__ void accept_kernel(Dims dm, SeqState st, Tree t, int batch, co
       if (emitted != nullptr) emitted[base + i] = -1;
     }
     __syncwarp();
-    const int L = st.L[b];
+    const int L = st.L[b], rows = st.nrow[b];                // (rows: the limits may have changed since the tree was verified)
     int next = 0, a = 0, last = 0;
     bool fin = false;
     const int* pred = force_pred != nullptr ? force_pred + base : t.pred + base;
-    if (st.nrow[b] > 0 && !st.done[b]) {
+    if (rows > 0 && !st.done[b]) {
       a = tr::walk_path(t.tok + base, t.par[0] + base, pred, N, lane, next, [&](int i, int node) {
-        if (fin) return;                                     // (lane 0: behind an accepted EOS)
+        if (fin || i >= rows) return;                        // (lane 0: behind an accepted EOS, or the last position; the next token is none's then)
         const int tok = t.tok[base + node];
         t.acc[base + node] = 1;
         st.hist[b * FM_HIST + ((L - 1 + i) & (FM_HIST - 1))] = tok;
