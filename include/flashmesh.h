@@ -451,7 +451,8 @@ int fm_device_status(fm_ctx* ctx);
 
 #define FM_MAX_TOP 32               /* alternatives per row of fm_logprobs                          */
 #define FM_MAX_TREE_NODES 256       /* nodes of one tree                                            */
-#define FM_MAX_SEQS 4096            /* sequences of one fm_pages, entries of one of its calls       */
+#define FM_MAX_SEQS 4096            /* sequences of one fm_pages, entries of one of its calls (of fm_pages_reserve and fm_pages_append
+                                     * as many as it has sequences: INVALID_ARG beyond) */
 #define FM_MAX_TREES 512            /* trees of one fm_tree_attention                               */
 #define FM_FILL_OUT 1
 #define FM_FILL_LSE 2
@@ -540,7 +541,9 @@ int fm_pages_compact(const fm_pages* pages, const fm_cache* cache, int32_t* used
  * than max_nodes nodes: CAPACITY in the status word, and the nodes behind take no part.  Offsets that are not inside the n_rows
  * rows: INVALID_ARG there.  Rows of such nodes, and those in front of row_off[0] and
  * behind row_off[n], are left as they were, or get what `fill` says.
- * Nothing is appended to the cache.  Errors: INVALID_ARG (null pointer, size, stride or alignment),
+ * Nothing is appended to the cache.  out may be q; it shares no memory with k_new, v_new or the cache.  max_nodes and max_len also
+ * choose between two kernels, for passes of few rows and of many: both are right at any size, bounds far above the
+ * sizes cost time.  Errors: INVALID_ARG (null pointer, size, stride or alignment),
  * UNSUPPORTED (head_dim not 64 / 128, dtype), CAPACITY (workspace, batch > FM_MAX_TREES, max_nodes > FM_MAX_TREE_NODES). */
 typedef struct fm_tree_args {
   const void* q;                    /* DEV [rows, n_heads, head_dim], rows q_row_stride apart        */

@@ -131,7 +131,7 @@ __device__ inline Seq sequence(const Args& a, int4 v) {
 
 // ---- the cut of all chunks into shares.  A tile counts OVER chunks more than it has: what starting and ending it takes.  (2, 4, 6, 8:
 // geometric means over 17 ragged and even batches of 97.5, 95.4, 94.1 and 95.3 us.)  A cut of up to NEAR chunks off the border
-// of a tile moves there; an eighth of a share in place of 3 chunks left some CTAs a quarter more than others (202 for 179 us
+// of a tile moves there; an eighth of a share in place of 3 chunks left some CTAs a quarter more than others (202 us for then 179
 // at 64 sequences of 4000 positions, 8 kv-heads of 128).
 constexpr int OVER = 6, NEAR = 3;
 struct Plan {
@@ -347,7 +347,7 @@ __device__ inline void fetch_ids(const Args& a, const Seq& s, const Chunk& k, in
   if (k.tree) return;
   const int* table = a.table + (int64_t)s.seq * a.max_pages;
   if (boxed(a, k)) {
-    const int rows = a.box_rows, slot = place_of(a, k.start + lane * rows), pi = a.page_div(slot);      // (at most C / 8 = 16 boxes)
+    const int rows = a.box_rows, slot = place_of(a, k.start + lane * rows), pi = a.page_div(slot);      // (boxes of 4 slots and more, 2 of a chunk of 64: a lane each)
     x.id[0] = lane * rows < k.n ? table[pi] : -1;
     x.in_page = slot - pi * a.page_div.d;
   } else {
@@ -512,8 +512,8 @@ __device__ inline void build_tree(Tree& t, const int* parent, int n, int tid, Sy
 // Eight warps multiply: four take the even chunks, four the odd ones, each a fixed slice of a chunk with its own running maximum,
 // sum and output (base 2).  At the end of a tile one of the two groups hands its states over and goes on, the other merges
 // and writes: they take turns.  Four warps load, queries and parents of the next tile included.
-// Bound: memory, once the SMs are full: 64 sequences of 4000 positions, 8 kv-heads of 128, one node: 179 us, 5.86 TB/s (89 % of a
-// copy); the same of 100 to 8000 positions in pages of 16: 103 us, 4.6 TB/s (70 %: pieces of 4 KB, parts and merges of ragged shares).
+// Bound: memory, once the SMs are full: 64 sequences of 4000 positions, 8 kv-heads of 128, one node: 176 us, 5.96 TB/s (91 % of a
+// copy); the same of 100 to 8000 positions in pages of 16: 102 us, 4.6 TB/s (70 %: pieces of 4 KB, parts and merges of ragged shares).
 // A pass of four nodes over 150 positions takes 8.6 us: a launch, the plan, a chunk's latency and the end of a tile.
 template <int DH>
 struct Rows16 {

@@ -189,7 +189,8 @@ class PagedCache:
 
         q [rows, heads, head_dim], k_new, v_new [rows, kv heads, head_dim] (rows may lie apart); row_off [n + 1]; parent [rows]: an earlier
         node of the tree, counted from its first row, or -1.  seqs [n]: the trees' sequences (None: 0 .. n-1).  max_nodes, max_len:
-        bounds on a tree's nodes and a sequence's positions (default: what there is room for).  Returns out, or (out, lse).
+        bounds on a tree's nodes and a sequence's positions (default: what there is room for).  They choose the kernel too: say them where they are
+        known, or single tokens of a batch are taken for one tree of many nodes.  Returns out, or (out, lse).
 
         A tree of more nodes than max_nodes, or than FM_MAX_TREE_NODES, is recorded for `check`; the nodes behind take no part.  So are offsets that do not
         ascend inside the rows.  Rows of no tree,

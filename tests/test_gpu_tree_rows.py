@@ -174,3 +174,15 @@ def test_accepted_offsets_that_are_not_inside_the_rows(off):
         at = slice(off[i], off[i + 1]) if fits(off, i) else slice(0, 0)
         want, behind = R.accept(tokens[at], parent[at], predicted[at])
         assert n_acc[i].item() == len(want) and nxt[i].item() == behind and path[i].tolist() == want + [-1] * (8 - len(want))
+
+
+@pytest.mark.parametrize("room", ["small", "large"])
+@pytest.mark.parametrize("dh,heads,Hkv", [(64, 4, 2), (128, 8, 1)])
+def test_outputs_in_the_place_of_the_queries(room, dh, heads, Hkv):
+    rng = np.random.default_rng(9)
+    lens, trees = [1500, 3, 260], [T.random_tree(rng, n) for n in (60, 1, 33)]
+    c, q, kn, vn = case(room, lens, trees, heads, Hkv, dh, 0, 9)
+    off, parent = T.dev(np.concatenate([[0], np.cumsum([len(t) for t in trees])])), T.dev(sum(trees, []))
+    want, lse = c.attention(0, q, kn, vn, off, parent, want_lse=True)
+    got, again = c.attention(0, q, kn, vn, off, parent, want_lse=True, out=q)
+    assert got.data_ptr() == q.data_ptr() and torch.equal(got, want) and torch.equal(again, lse)
