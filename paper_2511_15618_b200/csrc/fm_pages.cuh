@@ -191,6 +191,8 @@ __global__ void __launch_bounds__(PLAN) reserve_plan_kernel(const fm_pages p, co
     at[i] = total + block_scan(e < n ? want[i] : 0, sh, t);
     total += t;
   }
+  // Tables that could ask for 2^31 pages in one call: the sum may have left 32 bits.  All free pages are listed, and handed out entry by entry.
+  if ((int64_t)n * ((int64_t)p.max_pages + 1) > INT_MAX) total = INT_MAX;
   // the lowest `total` free ids
   int found = 0;
   for (int64_t p0 = 0; p0 < p.n_pages && found < total; p0 += 4 * PLAN) {
@@ -205,7 +207,7 @@ __global__ void __launch_bounds__(PLAN) reserve_plan_kernel(const fm_pages p, co
     found += t;
   }
   __syncthreads();
-  if (found < total) {                                       // not for all: entry by entry, in order
+  if (found < total) {                                       // not for all (or too many to add up): entry by entry, in order
     if (threadIdx.x != 0) return;
     int next = 0;
     for (int e = 0; e < n; ++e) {
