@@ -130,7 +130,8 @@ int score_rows(const lp::Args& a, cudaStream_t stream) {
   return launch(lp::long_kernel<T, 512, 8>, dim3(a.rows), 512, 8 * 512 * 16, stream, a);
 }
 
-// The form of a pass, by what the caller says of its sizes (bounds that are far above them take the other form: right, and slower).  Rows that share keys (nodes x heads of a group): up to 16 take tiles of
+// The form of a pass, by what the caller says of its sizes (bounds that are far above them take the other form: right, and
+// slower: 64 single tokens over 4000 positions each, called without bounds, 245 us for 176).  Rows that share keys (nodes x heads of a group): up to 16 take tiles of
 // 16 rows, warp-level products (a batch of 64, one node, 8 kv-heads of 128, 4000 positions: 176 us).  More rows would each have
 // the keys brought again, from L2 at best, so they take tensor-core tiles of 256 - but those start and end slower, and a tile
 // of 256 is one CTA's: passes too small to fill the SMs take the small tiles too.  Measured where a CTA has so many chunks
